@@ -298,6 +298,85 @@ HGA_API int hga_varlen_step(const hga_params* p, int32_t n_seq, const int32_t* c
 HGA_API int hga_varlen_workspace_bytes(const hga_params* p, int32_t n_seq, const int32_t* cu_q,
                                const int32_t* cu_k, size_t* bytes);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Paged key/value cache: where a program keeps the resident K and V of many sequences -- written token by token or chunk by
+ * chunk, as bf16 or quantised, read back as the dense tensors that the calls above take, and attended to exactly.  (The paper keeps
+ * its resident K/V in tiers and does not say how they are laid out; the layout, the formats and these calls are this library's.)
+ *
+ * The pool is K_cache and V_cache [n_pages, Hkv, page_size, row] (any order of the first three axes, by strides).  Sequence i's
+ * token at position t lies in row t % page_size of page block_table[i, t / page_size].  A row holds head_dim numbers:
+ *   HGA_CACHE_BF16   head_dim bf16
+ *   HGA_CACHE_MXFP8  head_dim bytes e4m3, and head_dim/32 scale bytes
+ *   HGA_CACHE_MXFP4  head_dim/2 bytes, two e2m1 each (the even element in the low half), and head_dim/32 scale bytes
+ * Scale byte s of a block of 32 consecutive elements stands for 2^(s - 127); a number is (element value) * 2^(s - 127).  hga_cache_write
+ * takes the smallest power, s >= 0, that brings the block's largest magnitude to the element type's largest value (448, 6) or
+ * below, and rounds each element once, to nearest, ties to even; so nothing saturates, and every number held is exactly a bf16 number.
+ * (Elements that would round to 2^128, past bf16's range, are rounded toward zero.)  A block with an infinity or a NaN gets s = 255
+ * and reads back as NaN.  K_scale, V_scale: uint8 [n_pages, Hkv, page_size, head_dim/32], dense; not used with HGA_CACHE_BF16.
+ *
+ * The calls of one step take the same description of it, in DEVICE memory, so that a captured step can be replayed with other
+ * contents:
+ *   cu_q         int32 [n_seq + 1]  prefix sums: the new tokens of sequence i are rows cu_q[i] .. cu_q[i+1]-1 of the packed
+ *                                   tensors (non-decreasing, cu_q[0] >= 0, cu_q[n_seq] <= n_tokens; rows outside are left alone)
+ *   seq_lens     int32 [n_seq]      resident tokens of each sequence INCLUDING its new ones, which are the last.  (Fewer than its
+ *                                   new tokens: the first of those have no place.  They are not written and see no key.)
+ *   block_table  int32 [n_seq, max_pages] (rows table_stride apart)
+ * Values that break these rules, or the limits max_new and max_len, fault nothing: HGA_STATUS_BAD_INDEX is set, and what lies outside
+ * the limits is left out.  An entry of block_table that is used and no page of the pool counts as a page of zeros; nothing is written
+ * to it.  A page that hga_cache_write writes to belongs to one sequence; pages that are only read may be shared. */
+#define HGA_CACHE_BF16 0
+#define HGA_CACHE_MXFP8 1
+#define HGA_CACHE_MXFP4 2
+
+typedef struct hga_cache_params {
+  int32_t n_seq, n_q_heads, n_kv_heads, head_dim; /* Hq % Hkv == 0, Hq/Hkv <= 128; head_dim in {64, 128}; n_seq <= 65535 */
+  int32_t page_size, n_pages, max_pages;          /* page_size a multiple of 8 in 8..4096; max_pages = entries of a
+                                                     block_table row                                             */
+  int32_t format;                                 /* HGA_CACHE_*                                                 */
+  int32_t n_tokens;                               /* rows of the packed tensors (all new tokens together)        */
+  int32_t max_new;                                /* no sequence has more new tokens than this (>= 1)            */
+  int32_t max_len;                                /* no seq_lens entry is larger than this; 0 = max_pages * page_size.  The
+                                                     closer, the better the work is shared out                    */
+  float   softmax_scale;                          /* <= 0 selects 1/sqrt(head_dim)                               */
+  int32_t flags;                                  /* 0                                                           */
+  int32_t reserved;                               /* 0                                                           */
+  /* element strides, all-zero meaning dense: (token, head) of Q, O, K_new, V_new; (page, head, token) of the pool, in bf16 elements
+   * or, quantised, in bytes; (sequence, head, token) of K_out and V_out.  Multiples of 8 bf16 elements, 16 bytes in
+   * quantised pools.  table_stride: 0 means max_pages */
+  int64_t q_stride[2], o_stride[2], kn_stride[2], vn_stride[2];
+  int64_t k_stride[3], v_stride[3], out_stride[3];
+  int64_t table_stride;
+} hga_cache_params;
+
+/* Writes the keys and values of the new tokens into the pool.  K_new, V_new bf16 [n_tokens, Hkv, d]; either pair (K_new with
+ * K_cache and K_scale, V_new with V_cache and V_scale) may be NULL.  Slots of no new token are left as they were. */
+HGA_API int hga_cache_write(const hga_cache_params* p, const void* K_new, const void* V_new, const int32_t* cu_q,
+                            const int32_t* seq_lens, const int32_t* block_table, void* K_cache, void* V_cache, void* K_scale,
+                            void* V_scale, int32_t* status_word, void* stream);
+
+/* Reads tokens [tok_begin, tok_end) of every sequence back as bf16, exactly: K_out, V_out [n_seq, Hkv, tok_end - tok_begin, d], the layout
+ * of the K and V that hga_build_summaries, hga_route and hga_attn_fwd take.  Rows of tokens at or behind seq_lens[i] are left as they
+ * were.  Either of K and V may be left out (NULL).  0 <= tok_begin <= tok_end.  cu_q is not needed. */
+HGA_API int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t tok_end, const int32_t* seq_lens,
+                           const int32_t* block_table, const void* K_cache, const void* V_cache, const void* K_scale,
+                           const void* V_scale, void* K_out, void* V_out, int32_t* status_word, void* stream);
+
+/* Exact softmax attention of the new tokens over the resident ones, causal among the new tokens: row t of sequence i, at
+ * position pos = seq_lens[i] - (cu_q[i+1] - cu_q[i]) + (t - cu_q[i]), attends to keys 0 .. pos (query head h to key/value head
+ * h / (Hq/Hkv)); hga_cache_write has put the new tokens' own keys there before.
+ *   Q, O bf16 [n_tokens, Hq, d]      LSE fp32 [n_tokens, Hq] (natural log; optional, may be NULL)
+ * A row that sees no key gets O = 0 and LSE = -inf.  Rows outside cu_q are left as they were.  Keys and values that a row does not
+ * see have no influence on it, not even infinities or NaN.  Products are of bf16 numbers (the cache's are), sums in fp32, the
+ * probabilities bf16; O is divided by the sum of the rounded ones.  Results do not depend on what else is in the batch, nor change from
+ * run to run, except that max_len, max_new and n_seq decide how the keys are shared out.
+ * workspace: device scratch of at least hga_cache_workspace_bytes() bytes (16-byte aligned; may be NULL where that is 0); contents
+ * are overwritten.  Calls that share a workspace must not overlap. */
+HGA_API int hga_cache_attn(const hga_cache_params* p, const void* Q, const int32_t* cu_q, const int32_t* seq_lens,
+                           const int32_t* block_table, const void* K_cache, const void* V_cache, const void* K_scale,
+                           const void* V_scale, void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                           int32_t* status_word, void* stream);
+HGA_API int hga_cache_workspace_bytes(const hga_cache_params* p, size_t* bytes);
+
 HGA_API const char* hga_status_string(int status);
 HGA_API int hga_version(void);
 /* the cudaError_t (as int) of the most recent failed CUDA call made by this library */
@@ -317,7 +396,10 @@ HGA_API int64_t hga_kernel_launch_count(void);
 #define HGA_KERNELS_BWD_TENSOR 5     /* hga_attn_bwd, tensor-core kernels (local band + routed sweep) */
 #define HGA_KERNELS_BWD_GENERIC 6    /* hga_attn_bwd, CUDA-core kernel */
 #define HGA_KERNELS_AUX 7            /* conversions (bf16 gradient outputs) and the self-test kernel */
-#define HGA_KERNELS_FAMILIES 8
+#define HGA_KERNELS_CACHE 8          /* hga_cache_write, hga_cache_read */
+#define HGA_KERNELS_CACHE_ROWS 9     /* hga_cache_attn, kernel for few query rows (and the join of its partial results) */
+#define HGA_KERNELS_CACHE_TENSOR 10  /* hga_cache_attn, tensor-core kernel for chunks */
+#define HGA_KERNELS_FAMILIES 11
 HGA_API int64_t hga_kernel_launch_count_by_family(int family);
 
 /* Self-test of the bounded on-chip waits (no counterpart in the paper).  Every wait on an mbarrier

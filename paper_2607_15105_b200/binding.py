@@ -32,12 +32,16 @@ EXPORTS = ("hga_build_summaries", "hga_route", "hga_route_static", "hga_attn_fwd
            "hga_workspace_bytes", "hga_layer_step", "hga_step_host", "hga_step_arena_bytes", "hga_tbptt_walk", "hga_varlen_step",
            "hga_varlen_workspace_bytes", "hga_status_string",
            "hga_version", "hga_last_cuda_error", "hga_kernel_launch_count", "hga_kernel_launch_count_by_family",
-           "hga_selftest_bounded_wait")
+           "hga_selftest_bounded_wait", "hga_cache_write", "hga_cache_read", "hga_cache_attn", "hga_cache_workspace_bytes")
 
 # kernel families of hga_kernel_launch_count_by_family
 (HGA_KERNELS_SUMMARIES, HGA_KERNELS_ROUTE_TENSOR, HGA_KERNELS_ROUTE_GENERIC, HGA_KERNELS_FWD_TENSOR,
- HGA_KERNELS_FWD_GENERIC, HGA_KERNELS_BWD_TENSOR, HGA_KERNELS_BWD_GENERIC, HGA_KERNELS_AUX) = range(8)
-HGA_KERNELS_FAMILIES = 8
+ HGA_KERNELS_FWD_GENERIC, HGA_KERNELS_BWD_TENSOR, HGA_KERNELS_BWD_GENERIC, HGA_KERNELS_AUX, HGA_KERNELS_CACHE,
+ HGA_KERNELS_CACHE_ROWS, HGA_KERNELS_CACHE_TENSOR) = range(11)
+HGA_KERNELS_FAMILIES = 11
+
+# element formats of the paged cache
+HGA_CACHE_BF16, HGA_CACHE_MXFP8, HGA_CACHE_MXFP4 = range(3)
 
 
 class HgaParams(C.Structure):
@@ -46,6 +50,15 @@ class HgaParams(C.Structure):
         "q_block", "topk_chunks", "topk_groups", "sink", "local")]
         + [("softmax_scale", C.c_float), ("flags", C.c_int32), ("summary_len", C.c_int32)]
         + [(n, C.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride", "o_stride")])
+
+
+class HgaCacheParams(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in (
+        "n_seq", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages", "format", "n_tokens", "max_new", "max_len")]
+        + [("softmax_scale", C.c_float), ("flags", C.c_int32), ("reserved", C.c_int32)]
+        + [(n, C.c_int64 * 2) for n in ("q_stride", "o_stride", "kn_stride", "vn_stride")]
+        + [(n, C.c_int64 * 3) for n in ("k_stride", "v_stride", "out_stride")]
+        + [("table_stride", C.c_int64)])
 
 
 class HgaError(RuntimeError):
@@ -89,6 +102,11 @@ def lib():
         L.hga_tbptt_walk.argtypes = [pp] + [vp] * 15 + [sz, vp, vp]
         L.hga_varlen_step.argtypes = [pp, C.c_int32] + [vp] * 17 + [sz, vp, vp]
         L.hga_varlen_workspace_bytes.argtypes = [pp, C.c_int32, vp, vp, C.POINTER(sz)]
+        pc = C.POINTER(HgaCacheParams)
+        L.hga_cache_write.argtypes = [pc] + [vp] * 11
+        L.hga_cache_read.argtypes = [pc, i32, i32] + [vp] * 10
+        L.hga_cache_attn.argtypes = [pc] + [vp] * 11 + [sz, vp, vp]
+        L.hga_cache_workspace_bytes.argtypes = [pc, C.POINTER(sz)]
         _lib = L
     return _lib
 
@@ -335,3 +353,51 @@ class HgaLayerBuffers:
         hga_layer_step(self.p, Q, K, V, dO, self.cfg.total_len - self.cfg.seg_len, self.cfg.total_len, self.chunk_sum, self.group_sum,
                        self.chunk_idx, self.group_idx, self.n_groups, self.chunk_scores, self.group_scores, self.O, self.LSE,
                        *bwd[:3], self.route_ws, bwd[3], self.status, stream)
+
+
+# ----------------------------------------------------------------------------- the paged key/value cache
+
+
+def make_cache_params(n_seq, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, fmt, n_tokens, max_new, max_len=0,
+                      softmax_scale=0.0, q_stride=None, o_stride=None, kn_stride=None, vn_stride=None, k_stride=None, v_stride=None,
+                      out_stride=None, table_stride=0) -> HgaCacheParams:
+    """hga_cache_params (see hga.h); strides in elements, or in bytes for the pool of a quantised format; None: dense."""
+    p = HgaCacheParams(n_seq, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, fmt, n_tokens, max_new, max_len,
+                       softmax_scale)
+    for name, s in (("q_stride", q_stride), ("o_stride", o_stride), ("kn_stride", kn_stride), ("vn_stride", vn_stride),
+                    ("k_stride", k_stride), ("v_stride", v_stride), ("out_stride", out_stride)):
+        if s is not None:
+            f = getattr(p, name)
+            f[:] = s
+    p.table_stride = table_stride
+    return p
+
+
+def hga_cache_workspace_bytes(p: HgaCacheParams) -> int:
+    n = C.c_size_t()
+    _check("hga_cache_workspace_bytes", lib().hga_cache_workspace_bytes(C.byref(p), C.byref(n)))
+    return n.value
+
+
+def hga_cache_write(p, K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale=None, V_scale=None, status_word=None,
+                    stream=None):
+    """Keys and values of the new tokens into the paged cache (see hga.h)."""
+    _check("hga_cache_write", lib().hga_cache_write(
+        C.byref(p), _ptr(K_new), _ptr(V_new), _ptr(cu_q), _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache),
+        _ptr(K_scale), _ptr(V_scale), _ptr(status_word), _stream(stream)))
+
+
+def hga_cache_read(p, tok_begin, tok_end, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, K_out, V_out, status_word=None,
+                   stream=None):
+    """Resident tokens [tok_begin, tok_end) of every sequence as dense bf16 (see hga.h)."""
+    _check("hga_cache_read", lib().hga_cache_read(
+        C.byref(p), tok_begin, tok_end, _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale),
+        _ptr(K_out), _ptr(V_out), _ptr(status_word), _stream(stream)))
+
+
+def hga_cache_attn(p, Q, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, O, LSE=None, workspace=None,
+                   status_word=None, stream=None):
+    """Exact attention of the new tokens over the paged cache (see hga.h)."""
+    _check("hga_cache_attn", lib().hga_cache_attn(
+        C.byref(p), _ptr(Q), _ptr(cu_q), _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale),
+        _ptr(O), _ptr(LSE), _ptr(workspace), _nbytes(workspace), _ptr(status_word), _stream(stream)))

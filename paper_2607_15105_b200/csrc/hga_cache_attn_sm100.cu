@@ -1,0 +1,628 @@
+// hga_cache_attn for chunks of new tokens (tcgen05 / TMEM / TMA).
+//
+// A unit is up to 256 query rows of one (sequence, key/value head) -- new tokens x query heads of the group, token by token -- as two
+// M-tiles of 128 rows, whose keys are taken in tiles of 128: S = Q K^T, P = 2^(S c - m), O += P V, with S, P and O in tensor memory.
+// The M-tiles take turns: while the softmax threads of one (four warps, a thread per row) work on S, the tensor pipe multiplies for
+// the other, so that neither waits.  Both read the same K and V tiles, which pass through one ring in shared memory.
+//
+//   warps 0-3, 4-7   softmax and epilogue of M-tile 0 and 1
+//   warp 8           issues the GEMMs
+//   warps 9, 10      copy K and V tiles by TMA, a box per page part (bf16 pages)
+//   warps 12-15      quantised pages: fetch, convert to bf16 and store K and V tiles; bf16 pages: clean the last V tiles
+//
+// A hidden key has weight zero, which does not silence a V row that is not finite.  So in the tiles that hold keys hidden from the
+// unit's first row (the last ones), numbers that are not finite are replaced by zeros, rows behind the last key altogether, and the
+// rows that do see such numbers get them added at the end.
+#include <algorithm>
+
+#include "hga_cache.cuh"
+#include "hga_sm100.cuh"
+
+namespace hga {
+
+using namespace sm100;
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kTile = 128;                 // rows of an M-tile, keys of a tile
+constexpr uint32_t kTmemCols = 512;
+constexpr float kNoRef = -1e30f;           // reference of a row that has seen no key: 2^(-inf - it) = 0
+// A row's reference is raised, and O rescaled, when a logit exceeds it by this much (log2): weights stay below 2^8, and most tiles
+// leave O alone.
+constexpr float kSlack = 8.f;
+
+template <int D>
+struct Smem {
+  static constexpr int kSlots = D == 128 ? 5 : 10;
+  static constexpr int kTileBytes = kTile * D * 2;
+  uint8_t q[2][kTileBytes];                // [panel of 64 elements][row][128 bytes], 128-byte swizzle, as all tiles
+  uint8_t ring[kSlots][kTileBytes];        // K and V tiles in turn
+  uint64_t full[kSlots], empty[kSlots];    // full: four arrivals, whoever fills the slot
+  uint64_t dirty[kSlots];                  // a V tile has arrived that has to be cleaned before it is full
+  uint64_t s_full[2], p_full[2], o_full[2], drain;
+  uint32_t tmem_base;
+  int abort, strange;
+  int seq, token0;                         // the unit's sequence, and its first token there
+};
+
+struct Plan {
+  int tokens;                              // of an M-tile
+  int units;                               // per key/value head and part, at most
+  int box;                                 // tokens of a TMA box: the largest power of two that divides the page (128 at most)
+  Div by_unit;                             // tokens of a unit
+  CacheSplit sp;
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// byte offset of 16-byte piece `c` of row r in a tile
+template <int D> __device__ __forceinline__ int piece(int r, int c) { return (c >> 3) * (kTile * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
+
+__device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort));
+}
+
+__device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7f80u) == 0x7f80u; }
+
+// The unit's place
+struct Unit {
+  CacheSeq s;
+  int seq, h, part, token0;
+  int pos0;                                // position of the sequence's first new token
+  int k0, k1;                              // keys of this part that some row sees
+  int first_lim;                           // last key that the unit's first row sees
+};
+
+template <int FMT, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheDims dm,
+                   const Plan plan, const uint16_t* __restrict__ Q, const int32_t* __restrict__ cu_q,
+                   const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table, const uint8_t* __restrict__ K,
+                   const uint8_t* __restrict__ V, const uint8_t* __restrict__ K_scale, const uint8_t* __restrict__ V_scale,
+                   uint16_t* __restrict__ O, float* __restrict__ LSE, float* __restrict__ part_o, int32_t* status_word) {
+  typedef Smem<D> Sm;
+  constexpr int NS = Sm::kSlots;
+  extern __shared__ uint8_t raw[];
+  Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int* abort = &sm.abort;
+
+  pdl_wait();
+  // Which sequence the unit lies in: units are counted off sequence after sequence, the last one first (late tokens see most keys, and
+  // long CTAs go first).  Units of one head follow one another, so that what runs at one time reads the same keys.
+  int at = blockIdx.x;
+  const int part = at % plan.sp.parts;  at /= plan.sp.parts;
+  const int h = at / plan.units, u = plan.units - 1 - (at - h * plan.units);
+  if (warp == 0) {
+    int seen = 0, seq = -1, t0 = 0;
+    bool bad = false;
+    const bool all = u == 0 && h == 0 && part == 0;      // (this CTA looks at every sequence, for the status word)
+    for (int i0 = 0; i0 < dm.n_seq && (seq < 0 || all); i0 += 32) {
+      const int i = i0 + lane;
+      int n = 0;
+      if (i < dm.n_seq) {
+        const CacheSeq s = cache_seq(dm, cu_q, seq_lens, i);
+        n = dm.n_tokens ? plan.by_unit(s.n + plan.tokens * 2 - 1) : 0;
+        bad = bad || s.bad;
+      }
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      const unsigned in = __ballot_sync(0xffffffffu, u < seen + upto);
+      if (in && seq < 0) {
+        const int l = __ffs(in) - 1;
+        seq = i0 + l;
+        t0 = (u - seen - __shfl_sync(0xffffffffu, upto - n, l)) * plan.tokens * 2;
+      }
+      seen += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (bad) cache_status(status_word, HGA_STATUS_BAD_INDEX);
+    if (lane == 0) { sm.seq = seq; sm.token0 = t0; }
+  }
+  if (tid == 32) {
+    sm.abort = sm.strange = 0;
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(&sm.full[i], 4);
+      mbar_init(&sm.empty[i], 1);
+      mbar_init(&sm.dirty[i], 1);
+    }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(&sm.s_full[x], 1);
+      mbar_init(&sm.p_full[x], 4);
+      mbar_init(&sm.o_full[x], 1);
+    }
+    mbar_init(&sm.drain, 1);
+    fence_barrier_init();
+  }
+  __syncthreads();
+  const int seq = sm.seq, token0 = sm.token0;
+  if (seq < 0) {                               // fewer units than there could be
+    pdl_launch_dependents();
+    return;
+  }
+  const CacheSeq s = cache_seq(dm, cu_q, seq_lens, seq);
+  const int pos0 = s.len - s.n_all;
+  const int n_tok = min(s.n - token0, 2 * plan.tokens);        // of the unit
+  const int first_lim = min(pos0 + token0, s.keys - 1), last_lim = min(pos0 + token0 + n_tok - 1, s.keys - 1);
+  const int k0 = part * plan.sp.keys, k1 = min(k0 + plan.sp.keys, last_lim + 1);
+  if (part > 0 && k0 >= k1) {
+    pdl_launch_dependents();
+    return;
+  }
+  // tiles of each M-tile (the first one's rows see fewer keys)
+  auto tiles_of = [&](int x) {
+    const int n = min(n_tok - x * plan.tokens, plan.tokens);
+    if (n <= 0) return 0;
+    const int end = min(k1, min(pos0 + token0 + x * plan.tokens + n - 1, s.keys - 1) + 1);
+    return max(end - k0 + kTile - 1, 0) / kTile;
+  };
+  const int n0 = tiles_of(0), n1 = tiles_of(1), n_tiles = max(n0, n1);
+
+  // Q, rows that are none as zeros
+  constexpr int C = D / 8;
+  for (int i = tid; i < 2 * kTile * C; i += kThreads) {
+    const int row = i / C, c = i % C, x = row / kTile, r = row % kTile;
+    const int t = dm.by_G(r), tok = x * plan.tokens + t;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (t < plan.tokens && tok < n_tok)
+      v = *reinterpret_cast<const uint4*>(Q + (s.q0 + token0 + tok) * dm.qs[0] + (h * dm.G + r - t * dm.G) * dm.qs[1] + c * 8);
+    *reinterpret_cast<uint4*>(sm.q[x] + piece<D>(r, c)) = v;
+  }
+  fence_proxy_async_smem();
+  if (warp == 8) {
+    tmem_alloc(&sm.tmem_base, kTmemCols);
+    tmem_relinquish();
+  }
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  if (tid == 0) pdl_launch_dependents();
+  const uint32_t tmem = sm.tmem_base;
+  // first tile with keys hidden from the unit's first row
+  const int first_dirty = max(first_lim + 1 - k0, 0) / kTile;
+
+  if (warp < 8) {
+    // ------------------------------------------------------------------ softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    const int x = warp >> 2, r = tid & 127;
+    const int t = dm.by_G(r), tok = x * plan.tokens + t;
+    const bool real = t < plan.tokens && tok < n_tok;
+    const int lim = real ? min(pos0 + token0 + tok, s.keys - 1) : 0x7fffffff;
+    const int head = h * dm.G + r - t * dm.G, row = s.q0 + token0 + tok;
+    const int n = x ? n1 : n0;
+    const int tile_lim = min(pos0 + token0 + x * plan.tokens, s.keys - 1);       // of the M-tile's first row
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + lanes + x * kTile, o_addr = tmem + lanes + 2 * kTile + x * D;
+    const float to_log2 = dm.scale * 1.44269504088896340736f;
+    const uint64_t to_log2_2 = pack_f32x2(to_log2, to_log2);
+    float m = kNoRef, l = 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int j = 0; j < n; ++j) {
+      ok = all_wait(&sm.s_full[x], j & 1, abort);
+      if (!ok) break;
+      tc_fence_after_sync();
+      uint32_t v[4][32];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tmem_ld32(s_addr + 32 * i, v[i]);
+      tmem_wait_ld();
+      const int base = k0 + j * kTile;
+      if (base + kTile - 1 > tile_lim) {
+        const int seen = lim - base;           // columns up to it are visible
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (32 * i + e > seen) v[i][e] = 0xff800000u;
+      }
+      float top[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        top[i] = __uint_as_float(v[i][0]);
+#pragma unroll
+        for (int e = 1; e < 32; ++e) top[i] = fmaxf(top[i], __uint_as_float(v[i][e]));
+      }
+      const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * to_log2;
+      if (__any_sync(0xffffffffu, mx > m + kSlack)) {
+        const float now = fmaxf(m, mx), f = fast_exp2(m - now);
+        m = now;
+        l *= f;
+        if (j > 0) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            uint32_t o[16];
+            tmem_ld16(o_addr + c, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st16(o_addr + c, o);
+          }
+        }
+      }
+      const uint64_t neg_m = pack_f32x2(-m, -m);
+      uint64_t sum = pack_f32x2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t p[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float a0, a1;
+          unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i][2 * e]), __uint_as_float(v[i][2 * e + 1])), to_log2_2, neg_m), a0, a1);
+          a0 = fast_exp2(a0);
+          a1 = fast_exp2(a1);
+          sum = add_f32x2(sum, pack_f32x2(a0, a1));
+          p[e] = pack_bf16(a0, a1);
+        }
+        tmem_st16(s_addr + 16 * i, p);
+      }
+      float s0, s1;
+      unpack_f32x2(sum, s0, s1);
+      l += s0 + s1;
+      tmem_wait_st();
+      tc_fence_before_sync();
+      mbar_arrive_warp(&sm.p_full[x]);
+    }
+    if (ok && n > 0) ok = all_wait(&sm.o_full[x], 0, abort);
+    __syncwarp();
+    __syncthreads();                           // every role is done: sm.strange and sm.abort are final
+    if (!*abort && n_tok > x * plan.tokens) {
+      tc_fence_after_sync();
+      const bool whole = s.keys <= plan.sp.keys;
+      const int64_t all_rows = (int64_t)dm.n_tokens * dm.Hq, out_row = (int64_t)row * dm.Hq + head;
+      const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);                // (NaN stays NaN)
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        __syncwarp();
+        if (n > 0) {
+          tmem_ld32(o_addr + c, o);
+          tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0;
+        }
+        if (!real) continue;
+        if (sm.strange) {
+          const int end = min(lim + 1, k1);
+          for (int key = max(first_lim + 1, k0); key < end; ++key) {
+            const int e0 = dm.by_page(key), pr = key - e0 * dm.page, page = table[seq * dm.table_stride + e0];
+            if (page < 0 || page >= dm.n_pages) continue;
+            if (FMT == kCacheBf16) {
+              const uint16_t* src = reinterpret_cast<const uint16_t*>(V) + page * dm.vs[0] + h * dm.vs[1] + pr * dm.vs[2] + c;
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (not_finite(src[e])) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float((uint32_t)src[e] << 16));
+            } else if (V_scale[(((int64_t)page * dm.Hkv + h) * dm.page + pr) * (D / 32) + (c >> 5)] == 255) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = 0x7fc00000u;
+            }
+          }
+        }
+        if (whole) {
+          uint4* dst = reinterpret_cast<uint4*>(O + row * dm.os[0] + head * dm.os[1] + c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = pack_bf16(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
+            dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        } else {
+          uint4* dst = reinterpret_cast<uint4*>(part_o + (part * all_rows + out_row) * D + c);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        }
+      }
+      if (real && whole && LSE) LSE[out_row] = l > 0.f ? (m + log2f(l)) * 0.69314718055994530942f : (l == 0.f ? -INFINITY : l);
+      if (real && !whole)
+        *reinterpret_cast<float4*>(part_o + plan.sp.parts * all_rows * D + (part * all_rows + out_row) * 4) = make_float4(m, l, l, 0.f);
+    }
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp == 8) {
+      // ---------------------------------------------------------------- GEMMs (the whole warp stays together, one lane issues)
+      const uint32_t lead = elect_one();
+      constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTile, 0, 0), idesc_o = idesc_bf16_f32(128, D, 0, 1);
+      const uint64_t q_desc = smem_desc_sw128(smem_u32(sm.q), 16, 1024);
+      const uint64_t k_desc = smem_desc_sw128(smem_u32(sm.ring), 16, 1024), v_desc = smem_desc_sw128(smem_u32(sm.ring), kTile * 128, 1024);
+      auto issue_s = [&](int x, int slot) {
+        const uint64_t a = desc_advance(q_desc, x * Sm::kTileBytes), b = desc_advance(k_desc, slot * Sm::kTileBytes);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          const uint32_t off = (i >> 2) * (kTile * 128) + (i & 3) * 32;
+          mma_ss_w(lead, tmem + x * kTile, desc_advance(a, off), desc_advance(b, off), idesc_s, i > 0);
+        }
+        mma_commit_w(lead, &sm.s_full[x]);
+      };
+      auto issue_pv = [&](int x, int slot, bool add) {
+        const uint64_t b = desc_advance(v_desc, slot * Sm::kTileBytes);
+#pragma unroll
+        for (int i = 0; i < kTile / 16; ++i)
+          mma_ts_w(lead, tmem + 2 * kTile + x * D, tmem + x * kTile + 8 * i, desc_advance(b, i * 2048), idesc_o, add || i > 0);
+      };
+      // position in the ring of K(j) is 2j, of V(j) 2j + 1
+      int slot = 0;
+      uint32_t phase = 0;
+      auto next = [&]() { if (++slot == NS) { slot = 0; phase ^= 1; } };
+      bool ok = true;
+      if (n_tiles > 0) {
+        ok = all_wait(&sm.full[0], 0, abort);
+        if (ok) {
+          tc_fence_after_sync();
+          if (n0 > 0) issue_s(0, 0);
+          if (n1 > 0) issue_s(1, 0);
+          mma_commit_w(lead, &sm.empty[0]);
+          next();
+        }
+      }
+#pragma unroll 1
+      for (int j = 0; ok && j < n_tiles; ++j) {
+        const int v_slot = slot;
+        ok = all_wait(&sm.full[v_slot], phase, abort);
+        next();
+        const bool more = j + 1 < n_tiles;
+        if (ok && more) ok = all_wait(&sm.full[slot], phase, abort);
+#pragma unroll 1
+        for (int x = 0; ok && x < 2; ++x) {
+          const int n = x ? n1 : n0;
+          if (j >= n) continue;
+          ok = all_wait(&sm.p_full[x], j & 1, abort);
+          if (!ok) break;
+          tc_fence_after_sync();
+          issue_pv(x, v_slot, j > 0);
+          if (j + 1 < n) issue_s(x, slot);
+          else mma_commit_w(lead, &sm.o_full[x]);
+        }
+        if (!ok) break;
+        mma_commit_w(lead, &sm.empty[v_slot]);
+        if (more) {
+          mma_commit_w(lead, &sm.empty[slot]);
+          next();
+        }
+      }
+    } else if (FMT == kCacheBf16 && warp < 11) {
+      // ---------------------------------------------------------------- copies of K (warp 9) and V (warp 10)
+      const bool is_v = warp == 10;
+      const CUtensorMap* map = is_v ? &map_v : &map_k;
+      const int boxes = kTile / plan.box, n_box = boxes * (D / 64);
+      bool bad = false;
+#pragma unroll 1
+      for (int j = 0; j < n_tiles; ++j) {
+        const int at_ring = 2 * j + is_v, use = at_ring / NS, slot = at_ring - use * NS;
+        if (!all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
+        uint64_t* bar = is_v && j >= first_dirty ? &sm.dirty[slot] : &sm.full[slot];
+        if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kTileBytes);
+        else if (lane < 4 && bar == &sm.full[slot]) mbar_arrive(bar);
+        __syncwarp();
+        if (lane < n_box) {
+          const int box = lane % boxes, panel = lane / boxes;
+          const int key = k0 + j * kTile + box * plan.box;
+          int page = dm.n_pages, r = 0;        // (a page behind the last one arrives as zeros)
+          if (key < k1) {
+            const int e = dm.by_page(key);
+            r = key - e * dm.page;
+            page = table[seq * dm.table_stride + e];
+            if (page < 0 || page >= dm.n_pages) { bad = true; page = dm.n_pages; }
+          }
+          tma_load_5d(sm.ring[slot] + panel * (kTile * 128) + box * plan.box * 128, map, bar, 0, r, panel, h, page);
+        }
+        __syncwarp();
+      }
+      if (bad) cache_status(status_word, HGA_STATUS_BAD_INDEX);
+      if (*abort && lane == 0) {
+        // giving up: give the copies still in flight time to land before shared memory is released
+        for (int it = 0; it < 64; ++it) __nanosleep(1000);
+      }
+    }
+    __syncwarp();
+    __syncthreads();
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    const int w = warp - 12;
+    bool strange = false;
+    if (FMT == kCacheBf16) {
+      // ---------------------------------------------------------------- V tiles with hidden keys: a thread per key
+      const int r = tid & 127;
+      uint32_t parity = 0;                     // of each slot's `dirty`
+#pragma unroll 1
+      for (int j = first_dirty; j < n_tiles; ++j) {
+        const int slot = (2 * j + 1) % NS;
+        if (!all_wait(&sm.dirty[slot], (parity >> slot) & 1, abort)) break;
+        parity ^= 1u << slot;
+        const int key = k0 + j * kTile + r;
+        if (key > first_lim) {
+#pragma unroll 4
+          for (int c = 0; c < C; ++c) {
+            uint4* at16 = reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, c));
+            if (key >= k1) {
+              *at16 = make_uint4(0, 0, 0, 0);
+              continue;
+            }
+            uint4 y = *at16;
+            uint32_t* e = &y.x;
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (not_finite(e[i])) { e[i] &= 0xffff0000u; odd = true; }
+              if (not_finite(e[i] >> 16)) { e[i] &= 0xffffu; odd = true; }
+            }
+            if (odd) { *at16 = y; strange = true; }
+          }
+        }
+        fence_proxy_async_smem();
+        mbar_arrive_warp(&sm.full[slot]);
+      }
+    } else {
+      // ---------------------------------------------------------------- quantised pages: fetched a tile ahead, converted, stored
+      constexpr int LPR = cache_row_bytes(FMT, D) / 16;        // lanes of a row, and 16-byte pieces that a thread has of a tile
+      constexpr int RPI = 32 / LPR;                            // rows of one load instruction
+      const int in_row = lane % LPR;
+      uint4 raw16[LPR];
+      uint32_t code[LPR];
+      bool bad = false;
+      int page_next = 0, row_next = 0;                         // of key octet `lane` (0-15) of the tile after the one in flight
+      auto look_up = [&](int j) {
+        const int key = k0 + j * kTile + (lane & 15) * 8;
+        page_next = -1;
+        if (key < k1) {
+          const int e = dm.by_page(key);
+          row_next = key - e * dm.page;
+          page_next = table[seq * dm.table_stride + e];
+          if (page_next < 0 || page_next >= dm.n_pages) { bad = true; page_next = -1; }
+        }
+      };
+      auto fetch = [&](int j, bool is_v) {
+        const uint8_t* src = is_v ? V : K;
+        const uint8_t* scales = is_v ? V_scale : K_scale;
+        const int64_t st0 = is_v ? dm.vs[0] : dm.ks[0], st1 = is_v ? dm.vs[1] : dm.ks[1], st2 = is_v ? dm.vs[2] : dm.ks[2];
+#pragma unroll
+        for (int i = 0; i < LPR; ++i) {
+          const int r = i * (4 * RPI) + w * RPI + lane / LPR, key = k0 + j * kTile + r;
+          const int page = __shfl_sync(0xffffffffu, page_next, r >> 3), pr = __shfl_sync(0xffffffffu, row_next, r >> 3) + (r & 7);
+          raw16[i] = make_uint4(0, 0, 0, 0);
+          code[i] = 127;
+          if (key < k1 && page >= 0) {
+            raw16[i] = __ldg(reinterpret_cast<const uint4*>(src + page * st0 + h * st1 + pr * st2 + in_row * 16));
+            code[i] = __ldg(scales + (((int64_t)page * dm.Hkv + h) * dm.page + pr) * (D / 32) + (FMT == kCacheMx8 ? in_row >> 1 : in_row));
+          }
+        }
+      };
+      if (n_tiles > 0) {
+        look_up(0);
+        fetch(0, false);
+      }
+#pragma unroll 1
+      for (int i_ring = 0; i_ring < 2 * n_tiles; ++i_ring) {
+        const int use = i_ring / NS, slot = i_ring - use * NS, j = i_ring >> 1;
+        const bool is_v = i_ring & 1;
+        if (!all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
+#pragma unroll
+        for (int i = 0; i < LPR; ++i) {
+          const int r = i * (4 * RPI) + w * RPI + lane / LPR;
+          uint32_t sc = code[i];
+          if (is_v && sc == 255 && k0 + j * kTile + r > first_lim) { sc = 0; strange = true; }
+          const uint32_t mul = pair(scale_bits(sc));
+          const uint32_t q[4] = {raw16[i].x, raw16[i].y, raw16[i].z, raw16[i].w};
+          if (FMT == kCacheMx8) {
+            uint32_t o[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              o[2 * k] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x1404)), kTwo120), mul);
+              o[2 * k + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x3424)), kTwo120), mul);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              *reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, 2 * in_row + k)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t o[4];
+              e2m1x4_to_bf16(q[k] & 0xffffu, o[0], o[1]);
+              e2m1x4_to_bf16(q[k] >> 16, o[2], o[3]);
+              *reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, 4 * in_row + k)) =
+                  make_uint4(mul_bf16x2(o[0], mul), mul_bf16x2(o[1], mul), mul_bf16x2(o[2], mul), mul_bf16x2(o[3], mul));
+            }
+          }
+        }
+        fence_proxy_async_smem();
+        mbar_arrive_warp(&sm.full[slot]);
+        if (i_ring + 1 < 2 * n_tiles) {
+          if (is_v) look_up(j + 1);
+          fetch(is_v ? j + 1 : j, !is_v);
+        }
+      }
+      if (bad) cache_status(status_word, HGA_STATUS_BAD_INDEX);
+    }
+    if (strange) sm.strange = 1;
+    __syncwarp();
+    __syncthreads();
+  }
+
+  // common exit
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (tid == 0 && sm.abort && status_word) atomicOr(status_word, HGA_STATUS_WAIT_TIMEOUT);
+  if (warp == 8) {
+    __syncwarp();
+    if (sm.abort) {
+      // given up: GEMMs already issued may still be writing tensor memory; wait (bounded) until the tensor pipe has run dry
+      mma_commit_w(elect_one(), &sm.drain);
+      mbar_wait(&sm.drain, 0);
+      __syncwarp();
+    }
+    tmem_dealloc(sm.tmem_base, kTmemCols);
+  }
+}
+
+Plan plan_of(const CacheDims& dm) {
+  Plan p;
+  p.tokens = kTile / dm.G;
+  p.by_unit = Div(2 * p.tokens);
+  p.box = 8;
+  while (p.box < kTile && dm.page % (2 * p.box) == 0) p.box *= 2;
+  // sum over the sequences of ceil(n / unit) <= tokens / unit + sequences; no sequence has more than max_new
+  const int64_t unit = 2 * p.tokens;
+  p.units = (int)std::min<int64_t>(dm.n_tokens / unit + std::min(dm.n_seq, dm.n_tokens), dm.n_seq * ((dm.max_new + unit - 1) / unit));
+  // Few units: their keys are shared out, so that the device is full
+  const int64_t ctas = (int64_t)p.units * dm.Hkv;
+  int64_t parts = ctas >= 148 ? 1 : (2 * 148 + ctas - 1) / ctas;
+  const int64_t keys = std::max<int64_t>((dm.max_keys + parts - 1) / parts, 512);
+  p.sp.keys = (int)std::min<int64_t>((keys + kTile - 1) / kTile * kTile, 0x7fffff00);
+  p.sp.parts = (int)std::max<int64_t>((dm.max_keys + p.sp.keys - 1) / p.sp.keys, 1);
+  return p;
+}
+
+template <int FMT, int D>
+int launch_of(const CacheDims& dm, const Plan& plan, const void* Q, const int32_t* cu_q, const int32_t* seq_lens, const int32_t* table,
+              const void* K, const void* V, const void* K_scale, const void* V_scale, void* O, float* LSE, void* workspace,
+              int32_t* status_word, cudaStream_t st) {
+  const int64_t ctas = (int64_t)plan.units * dm.Hkv * plan.sp.parts;
+  if (ctas > 0x7fffffff) return HGA_ERR_SHAPE;
+  CUtensorMap mk = {}, mv = {};
+  if (FMT == kCacheBf16) {
+    const uint32_t box[5] = {64, (uint32_t)plan.box, 1, 1, 1};
+    const uint64_t dims[5] = {64, (uint64_t)dm.page, (uint64_t)(D / 64), (uint64_t)dm.Hkv, (uint64_t)dm.n_pages};
+    const uint64_t sk[4] = {(uint64_t)dm.ks[2] * 2, 128, (uint64_t)dm.ks[1] * 2, (uint64_t)dm.ks[0] * 2};
+    const uint64_t sv[4] = {(uint64_t)dm.vs[2] * 2, 128, (uint64_t)dm.vs[1] * 2, (uint64_t)dm.vs[0] * 2};
+    if (encode_tensor_map_bf16(&mk, K, 5, dims, sk, box, true, false) || encode_tensor_map_bf16(&mv, V, 5, dims, sv, box, true, false))
+      return HGA_ERR_UNSUPPORTED;
+  }
+  auto* kernel = k_cache_attn_sm100<FMT, D>;
+  const size_t smem = sizeof(Smem<D>) + 1024;
+  static_assert(sizeof(Smem<D>) + 1024 <= 232448, "shared memory of a CTA");
+  const int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem, true);
+  if (rc) return rc;
+  PdlLaunch cfg(dim3((unsigned)ctas), kThreads, smem, st, 0);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg.c, kernel, mk, mv, dm, plan, (const uint16_t*)Q, cu_q, seq_lens, table, (const uint8_t*)K,
+                                           (const uint8_t*)V, (const uint8_t*)K_scale, (const uint8_t*)V_scale, (uint16_t*)O, LSE,
+                                           (float*)workspace, status_word);
+  count_launch(HGA_KERNELS_CACHE_TENSOR);
+  return record_cuda(e);
+}
+
+}  // namespace
+
+CacheSplit cache_tensor_split(const CacheDims& dm) { return plan_of(dm).sp; }
+
+int launch_cache_attn_sm100(const CacheDims& dm, const void* Q, const int32_t* cu_q, const int32_t* seq_lens, const int32_t* table,
+                            const void* K, const void* V, const void* K_scale, const void* V_scale, void* O, float* LSE, void* workspace,
+                            int32_t* status_word, cudaStream_t st) {
+  const Plan plan = plan_of(dm);
+#define HGA_TENSOR(F) (dm.d == 128 ? launch_of<F, 128> : launch_of<F, 64>)
+  auto* f = dm.format == kCacheBf16 ? HGA_TENSOR(kCacheBf16) : dm.format == kCacheMx8 ? HGA_TENSOR(kCacheMx8) : HGA_TENSOR(kCacheMx4);
+#undef HGA_TENSOR
+  const int rc = f(dm, plan, Q, cu_q, seq_lens, table, K, V, K_scale, V_scale, O, LSE, workspace, status_word, st);
+  if (rc || plan.sp.parts == 1) return rc;
+  return launch_cache_join(dm, plan.sp, cu_q, seq_lens, workspace, O, LSE, st);
+}
+
+}  // namespace hga

@@ -386,8 +386,9 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
 }  // namespace sm100
 
 // Host side: tensor-map encoding through the driver entry point (no link-time libcuda).
-// Returns 0 on success.  dims/strides innermost first; strides in bytes for dims 1..rank-1.
+// Returns 0 on success.  dims/strides innermost first; strides in bytes for dims 1..rank-1.  keep: look the map up among, and add it
+// to, those of earlier calls.
 int encode_tensor_map_bf16(CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
-                           const uint64_t* strides_bytes, const uint32_t* box, bool swizzle128);
+                           const uint64_t* strides_bytes, const uint32_t* box, bool swizzle128, bool keep = true);
 
 }  // namespace hga

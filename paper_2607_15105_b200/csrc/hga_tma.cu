@@ -50,7 +50,7 @@ constexpr size_t kMaxCachedMaps = 512;
 }  // namespace
 
 int encode_tensor_map_bf16(CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
-                           const uint64_t* strides_bytes, const uint32_t* box, bool swizzle128) {
+                           const uint64_t* strides_bytes, const uint32_t* box, bool swizzle128, bool keep) {
   auto enc = lookup_encoder();
   if (!enc) return -1;
   MapKey key;
@@ -64,7 +64,7 @@ int encode_tensor_map_bf16(CUtensorMap* out, const void* base, int rank, const u
     key.box[i] = box[i];
     if (i > 0) key.strides[i - 1] = strides_bytes[i - 1];
   }
-  {
+  if (keep) {
     std::lock_guard<std::mutex> lock(g_map_mutex);
     auto it = g_maps.find(key);
     if (it != g_maps.end()) { *out = it->second; return 0; }
@@ -83,6 +83,7 @@ int encode_tensor_map_bf16(CUtensorMap* out, const void* base, int rank, const u
                    swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return (int)r;
+  if (!keep) return 0;
   std::lock_guard<std::mutex> lock(g_map_mutex);
   if (g_maps.size() >= kMaxCachedMaps) g_maps.clear();
   g_maps.emplace(key, *out);
