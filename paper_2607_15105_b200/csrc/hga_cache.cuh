@@ -80,6 +80,18 @@ __device__ __forceinline__ void e2m1x4_to_bf16(uint32_t w, uint32_t& r0, uint32_
   r1 = __byte_perm(lo, hi, 0x7362) | ((w << 4) & 0x8000u) | ((w << 16) & 0x80000000u);
 }
 
+// Two e4m3 numbers (the low 16 bits) / two e2m1 numbers (the low 8 bits) as an fp16 pair, the lower one first
+__device__ __forceinline__ uint32_t e4m3x2_to_f16(uint32_t x) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t e2m1x2_to_f16(uint32_t x) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(r) : "r"(x));
+  return r;
+}
+
 constexpr int kCacheBf16 = HGA_CACHE_BF16, kCacheMx8 = HGA_CACHE_MXFP8, kCacheMx4 = HGA_CACHE_MXFP4;
 __host__ __device__ constexpr int cache_row_bytes(int fmt, int d) { return fmt == kCacheBf16 ? 2 * d : fmt == kCacheMx8 ? d : d / 2; }
 

@@ -64,7 +64,7 @@ static int resolve_cache(const hga_cache_params* p, CacheDims& dm) {
   return HGA_OK;
 }
 
-static bool few_rows(const CacheDims& dm) { return (int64_t)dm.max_new * dm.G <= 32; }
+static bool few_rows(const CacheDims& dm) { return (int64_t)dm.max_new * dm.G <= 64; }
 static CacheSplit attn_split(const CacheDims& dm) { return few_rows(dm) ? cache_rows_split(dm) : cache_tensor_split(dm); }
 
 }  // namespace hga

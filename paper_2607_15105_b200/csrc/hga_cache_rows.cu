@@ -1,21 +1,28 @@
 // hga_cache_attn for few query rows: generation steps, drafted tokens.
 //
 // A tile is up to 16 query rows of one (sequence, key/value head) -- new tokens x query heads of the group -- and a CTA takes a run
-// of keys for it.  Its four warps take 16 or 32 keys at a time, in turn, straight from global memory into the registers of warp-level
-// matrix instructions: nothing is shared between warps until the end, where their sums meet in shared memory.  What bounds it is the
-// keys' and values' bytes; tcgen05's 128-row tiles would be padding here.
+// of keys for it.  Its four warps take 16 or 32 keys at a time, in turn, each through a ring of its own in shared memory that
+// cp.async fills ahead, and work on them with warp-level matrix instructions: nothing is shared between warps until the end, where
+// their sums meet.  What bounds it is the keys' and values' bytes; tcgen05's 128-row tiles would be padding here.
 //
-// How the operands come about without a transposition: the order in which a product sums over its inner axis is free, and so is the
-// order of the columns of its result.  S = Q K^T: lane (g, c) = (lane / 4, lane % 4) of the instruction needs four numbers of key g
-// per 16 elements of the head dimension; it takes them from 16-byte pieces of the row of its own, and Q's registers are laid out for
-// the same order.  O^T = V^T P^T: P's registers are those of S as they are; a lane needs columns g of V for keys 2c, 2c+1, 2c+8, 2c+9
-// in pairs of keys, so it loads its share of the columns of these four rows and pairs them up by byte permutations.
+// How the operands come about: S = Q K^T; O^T = V^T P^T, because then P's registers are those of S as they are.  bf16: the registers
+// of K and (transposed) of V are what ldmatrix delivers.  Quantised: the order in which a product sums over its inner axis
+// is free, and so is the order of the rows of its result, so a lane (g, c) = (lane / 4, lane % 4) takes eight numbers of every
+// block of key g, and Q's registers are laid out for the same order; of V it takes the columns g D/8 .. of the keys 2c, 2c+1,
+// 2c+8, 2c+9 and pairs these up.
 //
-// Softmax: every warp has one reference per row, raised (and its sums rescaled) only when a logit exceeds it by 2^8, so that most
-// steps have no exchange between lanes.  LSE is of the exact probabilities; O is divided by the sum of the rounded ones, a
-// product with a column of ones.
+// Quantised pages are multiplied as fp16, into which the converter instructions go, and which holds e4m3 and e2m1 exactly.  K without
+// its scales: they multiply the sums over a block (fp32) afterwards; Q is brought to fp16 by a power of two per row, exactly but for
+// numbers 2^-29 of the row's largest.  V with its scales, times 2^kLift, where all of a step's lie in fp16's range (of blocks
+// between 2^-12 and 2^9 in magnitude, e4m3); other steps go through bf16, exactly too, and slower.
+//
+// Softmax: every warp has one reference per row, raised (and its sums rescaled) only when a logit exceeds it by 2^14, so that most
+// steps have no exchange between lanes.  It stays 2^6 below the row's largest when it is raised: fp16 then keeps weights down to 2^-31.
+// LSE is of the exact probabilities; O is divided by the sum of the rounded ones, a product with a column of ones.
 #include <algorithm>
-#include <cmath>
+#include <type_traits>
+
+#include <cuda_fp16.h>
 
 #include "hga_cache.cuh"
 #include "hga_sm100.cuh"
@@ -28,79 +35,147 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr float kNoRef = -1e30f;      // reference of a row without a key: 2^(-inf - it) = 0
-constexpr float kSlack = 8.f;         // log2 of how far a weight may exceed its reference's
+constexpr float kLow = 6.f, kSlack = 14.f;      // log2: how far the reference is set below the largest logit, and may be exceeded
 
-__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <bool kF16>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (kF16) mma_f16(d, a0, a1, a2, a3, b0, b1);
+  else mma_bf16(d, a0, a1, a2, a3, b0, b1);
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+__device__ __forceinline__ void mma_f16_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {      // d = a b
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// fp16 pairs that are bf16 numbers of few bits, as bf16 pairs
+__device__ __forceinline__ uint32_t f16_to_bf16(uint32_t x) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x));
+  return pack_bf16(f.x, f.y);
+}
 
-template <int W> __device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p) {
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {      // or zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <bool kTrans>
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  if (kTrans)
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+  else
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <int W>
+__device__ __forceinline__ void lds(uint32_t* w, const uint8_t* p) {
   if (W == 4) {
-    const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
     w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
   } else if (W == 2) {
-    const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
     w[0] = x.x; w[1] = x.y;
   } else {
-    w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
   }
 }
 
-// Where eight consecutive keys lie (page_size is a multiple of 8): byte offsets of the first one's rows, and its row of scales;
-// k < 0: no page of the pool
+// Where eight consecutive keys lie (page_size is a multiple of 8): the first one's rows, and its row of scales; k null: no page of the pool
 struct Octet {
-  int64_t k, v, s;
+  const uint8_t *k, *v;
+  int64_t s;
 };
 
-// A lane's share of a row of K (a quarter) and of V (an eighth): 16-byte pieces, the lanes' pieces next to one another
+// One warp's share of shared memory
 template <int FMT, int D>
-struct Share {
-  static constexpr int kRow = cache_row_bytes(FMT, D);
-  static constexpr int KW = kRow / 16, VW = kRow / 32;          // 32-bit words
-  static constexpr int KP = KW < 4 ? KW : 4, VP = VW < 4 ? VW : 4;      // words of a piece
-  // element of the head dimension that lane c's local element e of K is, e = 0 .. D/4 - 1
-  __device__ static __forceinline__ int k_element(int c, int e) {
-    constexpr int per = D / 4 / (KW / KP);
-    return (e / per) * 4 * per + c * per + e % per;
+struct Ring {
+  static constexpr int KS = FMT == kCacheBf16 ? 16 : 32;             // keys of a step
+  static constexpr int kRow = cache_row_bytes(FMT, D), NP = kRow / 16;      // bytes and 16-byte pieces of a row
+  static constexpr int kStages = 2;
+  static constexpr int NB = D / 32;                                  // blocks of a row
+  static constexpr int kScales = FMT == kCacheBf16 ? 0 : KS * NB;    // bytes
+  static constexpr int kStage = 2 * KS * kRow + 2 * kScales;         // K, V, their scales
+  static constexpr int kFactors = FMT == kCacheBf16 ? 0 : KS * NB * 6;      // K's scales as fp32 [key][block], V's as fp16 [block][key]
+  static constexpr int kBytes = kStages * kStage + kFactors;
+  // physical piece of piece p of row r, so that the accesses below meet no bank twice
+  __device__ static __forceinline__ int k_piece(int r, int p) {
+    if (FMT == kCacheBf16) return p ^ (r & 7);
+    if (NP == 8) return p ^ ((r & 3) << 1);
+    if (FMT == kCacheMx8) return p ^ (r & 2);
+    return NP == 4 ? p ^ ((r >> 1) & 3) : p ^ ((r >> 2) & 1);
   }
-  __device__ static __forceinline__ int v_element(int g, int e) {
-    constexpr int per = D / 8 / (VW / VP);
-    return (e / per) * 8 * per + g * per + e % per;
+  __device__ static __forceinline__ int v_piece(int r, int p) {
+    if (FMT == kCacheBf16) return p ^ (r & 7);
+    if (NP == 8) return p ^ (r & 6);
+    return NP == 4 ? p ^ (r & 2) : p;
   }
 };
 
-// the value of one element of the cache (for the few that are looked at one by one)
+// columns of O that rows g and g + 8 of product t are
+template <int FMT, int D>
+__device__ __forceinline__ int column(int g, int t, int half) {
+  return FMT == kCacheBf16 ? 16 * t + 8 * half + g : g * (D / 8) + 2 * t + half;
+}
+
+// the value of one element, where it is not finite
 template <int FMT>
-__device__ float one_value(const uint8_t* row, const uint8_t* scale, int e) {
+__device__ float strange_value(const uint8_t* row, const uint8_t* scale, int e) {
   if (FMT == kCacheBf16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[e] << 16);
-  return scale[e >> 5] == 255 ? __uint_as_float(0x7fc00000u) : 0.f;      // (finite ones are not asked for)
+  return scale[e >> 5] == 255 ? __uint_as_float(0x7fc00000u) : 0.f;
 }
 
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 4 : 3)
+__global__ void __launch_bounds__(kWarps * 32, FMT == kCacheMx4 && NT == 1 ? 4 : 3)
 k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* __restrict__ Q, const int32_t* __restrict__ cu_q,
              const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table, const uint8_t* __restrict__ K,
              const uint8_t* __restrict__ V, const uint8_t* __restrict__ K_scale, const uint8_t* __restrict__ V_scale,
              uint16_t* __restrict__ O, float* __restrict__ LSE, float* __restrict__ part_o, int32_t* status_word) {
-  typedef Share<FMT, D> Sh;
-  constexpr int kRowsTile = 8 * NT;
-  constexpr int KS = FMT == kCacheBf16 ? 16 : 32, SUB = KS / 16;       // keys a warp takes at once
+  typedef Ring<FMT, D> Rg;
+  constexpr int kRowsTile = 8 * NT, KS = Rg::KS, SUB = KS / 16, NB = Rg::NB;
   constexpr int kUnit = FMT == kCacheBf16 ? 2 : 1;
   constexpr int kPitch = D + 4;
-  typedef typename ScaleWord<D>::type SW;
+  constexpr bool kScaled = FMT != kCacheBf16;
+  // V's scales are 2^(code - 127 + kLift) as fp16; in range: 2^-14 .. 2^kTop
+  constexpr int kLift = FMT == kCacheMx8 ? 6 : FMT == kCacheMx4 ? 4 : 0, kTop = FMT == kCacheMx8 ? 7 : 13;
+  static_assert(kRowsTile * kPitch * 4 <= Rg::kBytes, "a warp's sums take the place of its ring");
   extern __shared__ __align__(16) uint8_t smem[];
   Octet* oct = reinterpret_cast<Octet*>(smem);                                     // [sp.keys / 8]
-  float* sm_o = reinterpret_cast<float*>(smem + (size_t)(sp.keys / 8) * sizeof(Octet));      // [kWarps][kRowsTile][kPitch]
   __shared__ float sm_m[kWarps][kRowsTile], sm_l[kWarps][kRowsTile], sm_r[kWarps][kRowsTile];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  uint8_t* const rings = smem + (size_t)(sp.keys / 8) * sizeof(Octet);
+  uint8_t* const ring = rings + warp * Rg::kBytes;
+  float* const k_factor = reinterpret_cast<float*>(ring + Rg::kStages * Rg::kStage);              // [KS][NB]
+  uint16_t* const v_factor = reinterpret_cast<uint16_t*>(k_factor + KS * NB);                     // [NB][KS]
   int at = blockIdx.x;
   const int mt = at % n_mt;  at /= n_mt;
   const int part = at % sp.parts;  at /= sp.parts;
@@ -120,78 +195,99 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
   if (part > 0 && k0 >= k1) return;
   const int nk = max(k1 - k0, 0);
 
+  bool all_there = true;
   for (int o = threadIdx.x; o < (nk + 7) / 8; o += kWarps * 32) {
     const int pos = k0 + o * 8, e = dm.by_page(pos), r = pos - e * dm.page;
     const int page = table[seq * dm.table_stride + e];
-    Octet x{-1, -1, 0};
+    Octet x{nullptr, nullptr, 0};
     if (page >= 0 && page < dm.n_pages) {
-      x.k = (page * dm.ks[0] + h * dm.ks[1] + r * dm.ks[2]) * kUnit;
-      x.v = (page * dm.vs[0] + h * dm.vs[1] + r * dm.vs[2]) * kUnit;
-      x.s = (((int64_t)page * dm.Hkv + h) * dm.page + r) * (D / 32);
+      x.k = K + (page * dm.ks[0] + h * dm.ks[1] + r * dm.ks[2]) * kUnit;
+      x.v = V + (page * dm.vs[0] + h * dm.vs[1] + r * dm.vs[2]) * kUnit;
+      x.s = (((int64_t)page * dm.Hkv + h) * dm.page + r) * NB;
     } else {
       cache_status(status_word, HGA_STATUS_BAD_INDEX);
+      all_there = false;
     }
     oct[o] = x;
   }
 
-  // Q in registers, in K's order; a row's last visible key
+  // Q in registers, in K's order; a row's last visible key; what its logits are multiplied by
   uint32_t qa[D / 16][2 * NT];
   int lim[NT];
+  float to_log2[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int row = row0 + n * 8 + g;
     const bool real = row < rows;
     const int t = real ? dm.by_G(row) : 0, head = h * dm.G + (row - t * dm.G);
     lim[n] = real ? min(pos0 + t, s.keys - 1) : 0x7fffffff;
+    to_log2[n] = dm.scale * 1.44269504088896340736f;
     const uint16_t* q = Q + (s.q0 + t) * dm.qs[0] + head * dm.qs[1];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      uint2 x = make_uint2(0, 0);
-      if (real) x = *reinterpret_cast<const uint2*>(q + Sh::k_element(c, 4 * i));
-      qa[i][2 * n] = x.x;
-      qa[i][2 * n + 1] = x.y;
+      qa[i][2 * n] = qa[i][2 * n + 1] = 0;
+      if (!real) continue;
+      if (kScaled) {
+        const uint2 x = *reinterpret_cast<const uint2*>(q + (i >> 1) * 32 + c * 8 + (i & 1) * 4);
+        qa[i][2 * n] = x.x;
+        qa[i][2 * n + 1] = x.y;
+      } else {
+        qa[i][2 * n] = *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * c);
+        qa[i][2 * n + 1] = *reinterpret_cast<const uint32_t*>(q + 16 * i + 8 + 2 * c);
+      }
+    }
+    if (kScaled) {
+      uint32_t big = 0;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int k = 2 * n; k < 2 * n + 2; ++k) big = max(big, max(qa[i][k] & 0x7fffu, (qa[i][k] >> 16) & 0x7fffu));
+      big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+      big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+      // the row's largest to 2^14 .. 2^15, by a power of two that fp32 holds (and its inverse)
+      const int up = max(min(127 + 14 - (int)(big >> 7), 100), -100);
+      const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+      to_log2[n] *= __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int k = 2 * n; k < 2 * n + 2; ++k)
+          qa[i][k] = pack_f16(__uint_as_float(qa[i][k] << 16) * f, __uint_as_float(qa[i][k] & 0xffff0000u) * f);
     }
   }
-  __syncthreads();
+  all_there = __syncthreads_and(all_there);
 
-  const int64_t k_lane = g * dm.ks[2] * kUnit + c * (Sh::KP * 4);
-  uint32_t kw[2 * SUB][Sh::KW], vw[4 * SUB][Sh::VW];
-  uint32_t ksc[2 * SUB], vsc[4 * SUB];
-
-  auto load_k = [&](int step) {
+  // Copies of one step: a lane's 16-byte pieces are those of number i * 32 + lane, row by row.  Keys past the end, and pages that are
+  // none, become zeros; steps without any need no test.
+  const uint32_t ring_addr = smem_u32(ring);
+  constexpr int kIter = KS * Rg::NP / 32, RPI = 32 / Rg::NP;             // copies of a lane, of K and of V; rows of a warp's
+  const int lr = lane / Rg::NP, lp = lane % Rg::NP;
+  const int64_t k_row = dm.ks[2] * kUnit, v_row = dm.vs[2] * kUnit;
+  const int64_t k_lane = (lr & 7) * k_row + lp * 16, v_lane = (lr & 7) * v_row + lp * 16;
+  constexpr int kPieces = KS * NB / 16;                                  // pieces of K's scales (eight keys have NB / 2), and of V's
+  auto fetch = [&](int step, int stage) {
+    const uint32_t dst = ring_addr + stage * Rg::kStage;
+    const Octet* first = oct + step * (KS / 8);
+    const bool whole = all_there && (step + 1) * KS <= nk;
 #pragma unroll
-    for (int u = 0; u < 2 * SUB; ++u) {
-      const int key = step * KS + u * 8;
-#pragma unroll
-      for (int i = 0; i < Sh::KW; ++i) kw[u][i] = 0;
-      ksc[u] = 0x7f7f7f7fu;
-      if (key + g < nk) {
-        const Octet x = oct[key >> 3];
-        if (x.k >= 0) {
-          const uint8_t* p = K + x.k + k_lane;
-#pragma unroll
-          for (int i = 0; i < Sh::KW / Sh::KP; ++i) load_words<Sh::KP>(&kw[u][i * Sh::KP], p + i * (16 * Sh::KP));
-          if (FMT != kCacheBf16) ksc[u] = __ldg(reinterpret_cast<const SW*>(K_scale + x.s + g * (D / 32)));
-        }
+    for (int i = 0; i < kIter; ++i) {
+      const int r = i * RPI + lr;
+      const Octet* x = first + i * RPI / 8 + (RPI > 8 ? lr >> 3 : 0);
+      const uint32_t k_dst = dst + r * Rg::kRow + Rg::k_piece(r, lp) * 16, v_dst = dst + (KS + r) * Rg::kRow + Rg::v_piece(r, lp) * 16;
+      if (whole) {
+        copy16(k_dst, x->k + k_lane + (i * RPI & 7) * k_row);
+        copy16(v_dst, x->v + v_lane + (i * RPI & 7) * v_row);
+      } else {
+        const bool there = step * KS + r < nk && x->k;
+        copy16(k_dst, there ? x->k + k_lane + (i * RPI & 7) * k_row : K, there);
+        copy16(v_dst, there ? x->v + v_lane + (i * RPI & 7) * v_row : V, there);
       }
     }
-  };
-  auto load_v = [&](int step) {
-#pragma unroll
-    for (int j = 0; j < 4 * SUB; ++j) {
-      const int key = step * KS + (j >> 1) * 8, in = 2 * c + (j & 1);
-#pragma unroll
-      for (int i = 0; i < Sh::VW; ++i) vw[j][i] = 0;
-      vsc[j] = 0x7f7f7f7fu;
-      if (key + in < nk) {
-        const Octet x = oct[key >> 3];
-        if (x.k >= 0) {
-          const uint8_t* p = V + x.v + in * dm.vs[2] * kUnit + g * (Sh::VP * 4);
-#pragma unroll
-          for (int i = 0; i < Sh::VW / Sh::VP; ++i) load_words<Sh::VP>(&vw[j][i * Sh::VP], p + i * (32 * Sh::VP));
-          if (FMT != kCacheBf16) vsc[j] = __ldg(reinterpret_cast<const SW*>(V_scale + x.s + in * (D / 32)));
-        }
-      }
+    if (kScaled && lane < 2 * kPieces) {
+      const int i = lane % kPieces, o8 = i / (NB / 2);
+      const Octet* x = first + o8;
+      const bool there = step * KS + o8 * 8 < nk && x->k;
+      copy16(dst + 2 * KS * Rg::kRow + lane * 16, (lane < kPieces ? K_scale : V_scale) + (there ? x->s + i % (NB / 2) * 16 : 0), there);
     }
   };
 
@@ -207,70 +303,131 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[n][t][i] = 0.f;
   }
-  const float to_log2 = dm.scale * 1.44269504088896340736f;
   bool strange = false;                 // a value hidden from some row of the tile is no finite number
   const int n_steps = (nk + KS - 1) / KS;
-  if (warp < n_steps) load_k(warp);
+  int ahead = warp, stage = 0;          // next step to fetch; stage of the step at hand
+#pragma unroll
+  for (int i = 0; i < Rg::kStages - 1; ++i) {
+    if (ahead < n_steps) fetch(ahead, i);
+    copies_commit();
+    ahead += kWarps;
+  }
 
 #pragma unroll 1
   for (int step = warp; step < n_steps; step += kWarps) {
-    load_v(step);
+    copies_wait<Rg::kStages - 2>();
+    __syncwarp();
+    // (every lane is done with the stage of the step before, which is filled next)
+    if (ahead < n_steps) fetch(ahead, stage == 0 ? Rg::kStages - 1 : stage - 1);
+    copies_commit();
+    ahead += kWarps;
+    uint8_t* const buf = ring + stage * Rg::kStage;
+    const uint8_t* const vbuf = buf + KS * Rg::kRow;
+    const uint32_t buf_addr = ring_addr + stage * Rg::kStage;
+    if (++stage == Rg::kStages) stage = 0;
+    const int base = k0 + step * KS;
+    const bool masked = base + KS - 1 > first_lim;
+
+    bool fits = true;                   // V's scales are in fp16's range
+    if (kScaled) {
+      // a lane prepares the scales of key `lane`
+      const uint8_t* sc = buf + 2 * KS * Rg::kRow;
+      uint32_t wk, wv;
+      if (NB == 4) {
+        wk = *reinterpret_cast<const uint32_t*>(sc + lane * 4);
+        wv = *reinterpret_cast<const uint32_t*>(sc + KS * NB + lane * 4);
+      } else {
+        wk = *reinterpret_cast<const uint16_t*>(sc + lane * 2);
+        wv = *reinterpret_cast<const uint16_t*>(sc + KS * NB + lane * 2);
+      }
+      float f[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        // (2^-127 becomes zero: such a block adds less than 2^-118 |q| to a logit)
+        f[b] = __uint_as_float(((wk >> (8 * b)) & 255u) << 23);
+        const uint32_t e = ((wv >> (8 * b)) & 255u) - (127 - kLift - 15);      // fp16's exponent field
+        fits = fits && e - 1 < kTop + 15;
+        v_factor[b * KS + lane] = (uint16_t)(e << 10);
+      }
+      // (a byte of 255: NaN)
+      if (((~wk - 0x01010101u) & wk & (NB == 4 ? 0x80808080u : 0x8080u)) != 0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          if (((wk >> (8 * b)) & 255u) == 255) f[b] = __uint_as_float(0x7fc00000u);
+      }
+      if (NB == 4) *reinterpret_cast<float4*>(k_factor + lane * 4) = make_float4(f[0], f[1], f[2 % NB], f[3 % NB]);
+      else *reinterpret_cast<float2*>(k_factor + lane * 2) = make_float2(f[0], f[1]);
+      fits = __all_sync(0xffffffffu, fits);
+      __syncwarp();
+    } else if (masked) {
+      // Values hidden from the first row: a weight of zero does not silence an infinity, so such numbers are left out here and given
+      // to the rows that see them at the end.
+      for (int i = lane; i < KS * Rg::NP; i += 32) {
+        const int r = i / Rg::NP;
+        if (base + r <= first_lim) continue;
+        uint4* y = reinterpret_cast<uint4*>(buf + KS * Rg::kRow + i * 16);
+        uint4 x = *y;
+        uint32_t* w = &x.x;
+        bool odd = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if ((w[k] & 0x7f80u) == 0x7f80u) { w[k] &= 0xffff0000u; odd = true; }
+          if ((w[k] & 0x7f800000u) == 0x7f800000u) { w[k] &= 0xffffu; odd = true; }
+        }
+        if (odd) { *y = x; strange = true; }
+      }
+      __syncwarp();
+    }
+
     float x[2 * SUB][4];
 #pragma unroll
     for (int u = 0; u < 2 * SUB; ++u) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[u][i] = 0.f;
+      if (!kScaled) {
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        uint32_t b0, b1;
-        if (FMT == kCacheBf16) {
-          b0 = kw[u][(2 * i) % Sh::KW];
-          b1 = kw[u][(2 * i + 1) % Sh::KW];
-        } else if (FMT == kCacheMx8) {
-          // block of piece i / 4 (16 bytes): 2 (i / 4) + c / 2
-          const uint32_t mul = pair(scale_bits((ksc[u] >> (8 * (2 * (i / 4) + (c >> 1)))) & 255u));
-          b0 = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(kw[u][i % Sh::KW], 0, 0x1404)), kTwo120), mul);
-          b1 = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(kw[u][i % Sh::KW], 0, 0x3424)), kTwo120), mul);
-        } else {
-          const uint32_t mul = pair(scale_bits((ksc[u] >> (8 * (D == 128 ? c : c >> 1))) & 255u));
-          e2m1x4_to_bf16((i & 1) ? kw[u][(i / 2) % Sh::KW] >> 16 : kw[u][(i / 2) % Sh::KW] & 0xffffu, b0, b1);
-          b0 = mul_bf16x2(b0, mul);
-          b1 = mul_bf16x2(b1, mul);
+        for (int i = 0; i < D / 32; ++i) {        // 32 elements: four 8 x 8 matrices of keys u * 8 ..
+          uint32_t b[4];
+          ldmatrix4<false>(b, buf_addr + (u * 8 + (lane & 7)) * Rg::kRow + Rg::k_piece(lane & 7, 4 * i + (lane >> 3)) * 16);
+          mma_bf16(x[u], qa[2 * i][0], NT == 2 ? qa[2 * i][2 % (2 * NT)] : 0u, qa[2 * i][1], NT == 2 ? qa[2 * i][3 % (2 * NT)] : 0u, b[0], b[1]);
+          mma_bf16(x[u], qa[2 * i + 1][0], NT == 2 ? qa[2 * i + 1][2 % (2 * NT)] : 0u, qa[2 * i + 1][1],
+                   NT == 2 ? qa[2 * i + 1][3 % (2 * NT)] : 0u, b[2], b[3]);
         }
-        mma_16816(x[u], qa[i][0], NT == 2 ? qa[i][2 % (2 * NT)] : 0u, qa[i][1], NT == 2 ? qa[i][3 % (2 * NT)] : 0u, b0, b1);
+      } else {
+        float f0[NB], f1[NB];                     // of keys 2c, 2c + 1
+        lds<NB>(reinterpret_cast<uint32_t*>(f0), reinterpret_cast<const uint8_t*>(k_factor + (u * 8 + 2 * c) * NB));
+        lds<NB>(reinterpret_cast<uint32_t*>(f1), reinterpret_cast<const uint8_t*>(k_factor + (u * 8 + 2 * c + 1) * NB));
+        const int r = u * 8 + g;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          float acc[4];
+          uint32_t k[4];
+          if (FMT == kCacheMx8) {
+            uint32_t w[2];
+            lds<2>(w, buf + r * Rg::kRow + Rg::k_piece(r, 2 * b + (c >> 1)) * 16 + (c & 1) * 8);
+            k[0] = e4m3x2_to_f16(w[0]); k[1] = e4m3x2_to_f16(w[0] >> 16);
+            k[2] = e4m3x2_to_f16(w[1]); k[3] = e4m3x2_to_f16(w[1] >> 16);
+          } else {
+            uint32_t w;
+            lds<1>(&w, buf + r * Rg::kRow + Rg::k_piece(r, b) * 16 + c * 4);
+            k[0] = e2m1x2_to_f16(w); k[1] = e2m1x2_to_f16(w >> 8); k[2] = e2m1x2_to_f16(w >> 16); k[3] = e2m1x2_to_f16(w >> 24);
+          }
+          mma_f16_zero(acc, qa[2 * b][0], NT == 2 ? qa[2 * b][2 % (2 * NT)] : 0u, qa[2 * b][1], NT == 2 ? qa[2 * b][3 % (2 * NT)] : 0u, k[0], k[1]);
+          mma_f16(acc, qa[2 * b + 1][0], NT == 2 ? qa[2 * b + 1][2 % (2 * NT)] : 0u, qa[2 * b + 1][1],
+                  NT == 2 ? qa[2 * b + 1][3 % (2 * NT)] : 0u, k[2], k[3]);
+#pragma unroll
+          for (int i = 0; i < 2 * NT; ++i) x[u][i] = fmaf(acc[i], (i & 1) ? f1[b] : f0[b], x[u][i]);
+        }
       }
     }
-    if (step + kWarps < n_steps) load_k(step + kWarps);
 
-    // logits in units of log2, hidden ones -inf
-#pragma unroll
-    for (int u = 0; u < 2 * SUB; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[u][i] *= to_log2;
-    const int base = k0 + step * KS;
-    if (base + KS - 1 > first_lim) {
+    // hidden logits -inf
+    if (masked) {
 #pragma unroll
       for (int u = 0; u < 2 * SUB; ++u)
 #pragma unroll
         for (int i = 0; i < 2 * NT; ++i)
           if (base + u * 8 + 2 * c + (i & 1) > lim[i >> 1] || base + u * 8 + 2 * c + (i & 1) >= k1) x[u][i] = -INFINITY;
-      // values hidden from the first row: a weight of zero does not silence an infinity, so such numbers are left out here and
-      // given to the rows that see them at the end
-#pragma unroll
-      for (int j = 0; j < 4 * SUB; ++j) {
-        if (base + (j >> 1) * 8 + 2 * c + (j & 1) <= first_lim) continue;
-        if (FMT == kCacheBf16) {
-#pragma unroll
-          for (int i = 0; i < Sh::VW; ++i) {
-            if ((vw[j][i] & 0x7f80u) == 0x7f80u) { vw[j][i] &= 0xffff0000u; strange = true; }
-            if ((vw[j][i] & 0x7f800000u) == 0x7f800000u) { vw[j][i] &= 0xffffu; strange = true; }
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < D / 32; ++i)
-            if (((vsc[j] >> (8 * i)) & 255u) == 255u) { vsc[j] &= ~(255u << (8 * i)); strange = true; }
-        }
-      }
     }
     float top[NT];
     bool raise = false;
@@ -279,14 +436,16 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
       top[n] = x[0][2 * n];
 #pragma unroll
       for (int u = 0; u < 2 * SUB; ++u) top[n] = fmaxf(top[n], fmaxf(x[u][2 * n], x[u][2 * n + 1]));
+      top[n] *= to_log2[n];             // (in units of log2)
       raise = raise || top[n] > m[n] + kSlack;
     }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float now = fmaxf(m[n], top[n]);
+        float now = top[n];
         now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 1));
         now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 2));
+        now = fmaxf(m[n], now - kLow);
         const float f = fast_exp2(m[n] - now);
         m[n] = now;
         l[n] *= f;
@@ -299,72 +458,116 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
           for (int i = 0; i < 4; ++i) o[n][t][i] *= (i & 1) ? f1 : f0;
       }
     }
-    uint32_t p[NT][2 * SUB];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int u = 0; u < 2 * SUB; ++u)
 #pragma unroll
-      for (int u = 0; u < 2 * SUB; ++u) {
-        const float p0 = fast_exp2(x[u][2 * n] - m[n]), p1 = fast_exp2(x[u][2 * n + 1] - m[n]);
-        l[n] += p0 + p1;
-        p[n][u] = pack_bf16(p0, p1);
+      for (int n = 0; n < NT; ++n) {
+        x[u][2 * n] = fast_exp2(fmaf(x[u][2 * n], to_log2[n], -m[n]));
+        x[u][2 * n + 1] = fast_exp2(fmaf(x[u][2 * n + 1], to_log2[n], -m[n]));
+        l[n] += x[u][2 * n] + x[u][2 * n + 1];
       }
-#pragma unroll
-    for (int b = 0; b < SUB; ++b) {
-      uint32_t mul01 = 0, mul23 = 0;
-      if (FMT != kCacheBf16) {
-        const int sh = 8 * (D == 128 ? g >> 1 : g >> 2);
-        mul01 = scale_bits((vsc[4 * b] >> sh) & 255u) | (scale_bits((vsc[4 * b + 1] >> sh) & 255u) << 16);
-        mul23 = scale_bits((vsc[4 * b + 2] >> sh) & 255u) | (scale_bits((vsc[4 * b + 3] >> sh) & 255u) << 16);
-      }
+
+    if (!kScaled) {
+      uint32_t p[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        mma_16816(ones[n], 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, p[n][2 * b], p[n][2 * b + 1]);
 #pragma unroll
-      for (int t = 0; t < D / 16; ++t) {      // local columns 2t, 2t + 1
+        for (int u = 0; u < 2; ++u) p[n][u] = pack_bf16(x[u][2 * n], x[u][2 * n + 1]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) mma_bf16(ones[n], 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, p[n][0], p[n][1]);
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) {
+        // (keys 0-7, columns 16t ..), (same, 16t + 8 ..), (keys 8-15, 16t ..), (same, 16t + 8 ..), transposed
         uint32_t a[4];
+        const int r = (lane & 7) + ((lane >> 4) << 3);
+        ldmatrix4<true>(a, buf_addr + KS * Rg::kRow + r * Rg::kRow + Rg::v_piece(r, 2 * t + ((lane >> 3) & 1)) * 16);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t* w0 = vw[4 * b + 2 * half];
-          const uint32_t* w1 = vw[4 * b + 2 * half + 1];
-          if (FMT == kCacheBf16) {
-            a[2 * half] = __byte_perm(w0[t % Sh::VW], w1[t % Sh::VW], 0x5410);
-            a[2 * half + 1] = __byte_perm(w0[t % Sh::VW], w1[t % Sh::VW], 0x7632);
-          } else if (FMT == kCacheMx8) {
-            const uint32_t mul = half ? mul23 : mul01;
-            const uint32_t u0 = w0[(t / 2) % Sh::VW], u1 = w1[(t / 2) % Sh::VW];
-            a[2 * half] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(u0, u1, (t & 1) ? 0x6420 : 0x4400)), kTwo120), mul);
-            a[2 * half + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(u0, u1, (t & 1) ? 0x7430 : 0x5410)), kTwo120), mul);
-          } else {
-            const uint32_t mul = half ? mul23 : mul01;
-            const uint32_t u0 = w0[(t / 4) % Sh::VW], u1 = w1[(t / 4) % Sh::VW];
-            const uint32_t even = (u0 & 0x0f0f0f0fu) | ((u1 << 4) & 0xf0f0f0f0u), odd = ((u0 >> 4) & 0x0f0f0f0fu) | (u1 & 0xf0f0f0f0u);
-            uint32_t e0, e1, d0, d1;
-            e2m1x4_to_bf16((t & 2) ? even >> 16 : even & 0xffffu, e0, e1);
-            e2m1x4_to_bf16((t & 2) ? odd >> 16 : odd & 0xffffu, d0, d1);
-            a[2 * half] = mul_bf16x2((t & 1) ? e1 : e0, mul);
-            a[2 * half + 1] = mul_bf16x2((t & 1) ? d1 : d0, mul);
+        for (int n = 0; n < NT; ++n) mma_bf16(o[n][t], a[0], a[1], a[2], a[3], p[n][0], p[n][1]);
+      }
+    } else {
+      constexpr int VW = Rg::kRow / 32;           // 32-bit words of a lane's share of a row of V
+      const int block = g * NB / 8;
+      auto weigh = [&](auto as_f16) {
+        constexpr bool kF16 = decltype(as_f16)::value;
+#pragma unroll
+        for (int b = 0; b < SUB; ++b) {
+          uint32_t w[4][VW], p[NT][2], mul[2];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = b * 16 + (j >> 1) * 8 + 2 * c + (j & 1), byte = g * 4 * VW;
+            lds<VW>(w[j], vbuf + r * Rg::kRow + Rg::v_piece(r, byte >> 4) * 16 + (byte & 15));
+          }
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int r = b * 16 + half * 8 + 2 * c;
+            if (kF16) {
+              mul[half] = *reinterpret_cast<const uint32_t*>(v_factor + block * KS + r);
+            } else {
+              // the scales as they are; the lift comes in by P
+              const uint8_t* sc = buf + 2 * KS * Rg::kRow + KS * NB;
+              uint32_t s0 = sc[r * NB + block], s1 = sc[(r + 1) * NB + block];
+              // (NaN, hidden from some row: see above)
+              if (s0 == 255 && base + r > first_lim) { s0 = 0; strange = true; }
+              if (s1 == 255 && base + r + 1 > first_lim) { s1 = 0; strange = true; }
+              mul[half] = scale_bits(s0) | (scale_bits(s1) << 16);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              p[n][u] = kF16 ? pack_f16(x[2 * b + u][2 * n], x[2 * b + u][2 * n + 1]) : pack_bf16(x[2 * b + u][2 * n], x[2 * b + u][2 * n + 1]);
+            constexpr uint32_t one = kF16 ? 0x3c003c00u : 0x3f803f80u;
+            mma<kF16>(ones[n], one, one, one, one, p[n][0], p[n][1]);
+            if (!kF16)
+              for (int u = 0; u < 2; ++u) p[n][u] = mul_bf16x2(p[n][u], pack_bf16((float)(1 << kLift), (float)(1 << kLift)));
+          }
+#pragma unroll
+          for (int t2 = 0; t2 < D / 32; ++t2) {      // local columns 4 t2 .. 4 t2 + 3
+            uint32_t a[2][4];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const uint32_t u0 = w[2 * half][t2 / (FMT == kCacheMx8 ? 1 : 2)], u1 = w[2 * half + 1][t2 / (FMT == kCacheMx8 ? 1 : 2)];
+              uint32_t y[4];
+              if (FMT == kCacheMx8) {
+                const uint32_t lo = __byte_perm(u0, u1, 0x5140), hi = __byte_perm(u0, u1, 0x7362);
+                y[0] = e4m3x2_to_f16(lo); y[1] = e4m3x2_to_f16(lo >> 16); y[2] = e4m3x2_to_f16(hi); y[3] = e4m3x2_to_f16(hi >> 16);
+              } else {
+                const uint32_t even = (u0 & 0x0f0f0f0fu) | ((u1 << 4) & 0xf0f0f0f0u), odd = ((u0 >> 4) & 0x0f0f0f0fu) | (u1 & 0xf0f0f0f0u);
+                const int sh = (t2 & 1) * 16;
+                y[0] = e2m1x2_to_f16(even >> sh); y[1] = e2m1x2_to_f16(odd >> sh);
+                y[2] = e2m1x2_to_f16(even >> (sh + 8)); y[3] = e2m1x2_to_f16(odd >> (sh + 8));
+              }
+#pragma unroll
+              for (int k = 0; k < 4; ++k) a[k >> 1][2 * half + (k & 1)] = kF16 ? mul_f16x2(y[k], mul[half]) : mul_bf16x2(f16_to_bf16(y[k]), mul[half]);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int n = 0; n < NT; ++n) mma<kF16>(o[n][2 * t2 + k], a[k][0], a[k][1], a[k][2], a[k][3], p[n][0], p[n][1]);
           }
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma_16816(o[n][t], a[0], a[1], a[2], a[3], p[n][2 * b], p[n][2 * b + 1]);
-      }
+      };
+      if (fits) weigh(std::true_type{});
+      else weigh(std::false_type{});
     }
   }
+  copies_wait<0>();
+  __syncwarp();
 
-  // the warps' sums meet
+  // the warps' sums meet (each warp's in the place of its ring)
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
     l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
     if (c == 0) { sm_m[warp][n * 8 + g] = m[n]; sm_l[warp][n * 8 + g] = l[n]; }
     if (g == 0) { sm_r[warp][n * 8 + 2 * c] = ones[n][0]; sm_r[warp][n * 8 + 2 * c + 1] = ones[n][1]; }
-    float* dst = sm_o + (size_t)(warp * kRowsTile + n * 8 + 2 * c) * kPitch;
+    float* dst = reinterpret_cast<float*>(ring) + (n * 8 + 2 * c) * kPitch;
+    constexpr float down = 1.f / (float)(1 << kLift);
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) {
-      const int col = Sh::v_element(g, 2 * t);
-      *reinterpret_cast<float2*>(dst + col) = make_float2(o[n][t][0], o[n][t][2]);
-      *reinterpret_cast<float2*>(dst + kPitch + col) = make_float2(o[n][t][1], o[n][t][3]);
-    }
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dst[(i & 1) * kPitch + column<FMT, D>(g, t, i >> 1)] = o[n][t][i] * down;
   }
   const bool any_strange = __syncthreads_or(strange);
   const bool whole = s.keys <= sp.keys;                  // the sequence is one part
@@ -381,7 +584,7 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       const float f = fast_exp2(sm_m[w][r] - top);
-      const float4 x = *reinterpret_cast<const float4*>(sm_o + (size_t)(w * kRowsTile + r) * kPitch + col);
+      const float4 x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(rings + w * Rg::kBytes) + r * kPitch + col);
       sum.x += f * x.x; sum.y += f * x.y; sum.z += f * x.z; sum.w += f * x.w;
       ls += f * sm_l[w][r];
       lr += f * sm_r[w][r];
@@ -391,14 +594,14 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
       const int end = min(min(pos0 + t, s.keys - 1) + 1, k1);
       for (int key = max(first_lim + 1, k0); key < end; ++key) {
         const Octet x = oct[(key - k0) >> 3];
-        if (x.k < 0) continue;
+        if (!x.k) continue;
         const int in = (key - k0) & 7;
-        const uint8_t* vr = V + x.v + in * dm.vs[2] * kUnit;
+        const uint8_t* vr = x.v + in * dm.vs[2] * kUnit;
         const uint8_t* sr = V_scale + x.s + in * (D / 32);
         float* e = &sum.x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float y = one_value<FMT>(vr, sr, col + i);
+          const float y = strange_value<FMT>(vr, sr, col + i);
           if (!isfinite(y)) e[i] += y;
         }
       }
@@ -474,7 +677,7 @@ int rows_of(const CacheDims& dm, const CacheSplit& sp, const void* Q, const int3
   const int n_mt = (dm.max_new * dm.G + 8 * NT - 1) / (8 * NT);
   const int64_t ctas = (int64_t)dm.n_seq * dm.Hkv * sp.parts * n_mt;
   if (ctas > 0x7fffffff) return HGA_ERR_SHAPE;
-  const size_t smem = (size_t)(sp.keys / 8) * sizeof(Octet) + (size_t)kWarps * 8 * NT * (D + 4) * sizeof(float);
+  const size_t smem = (size_t)(sp.keys / 8) * sizeof(Octet) + (size_t)kWarps * Ring<FMT, D>::kBytes;
   auto* kernel = k_cache_rows<FMT, D, NT>;
   const int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem, true);
   if (rc) return rc;
@@ -494,7 +697,7 @@ CacheSplit cache_rows_split(const CacheDims& dm) {
   const int64_t tiles = (int64_t)dm.n_seq * dm.Hkv * ((dm.max_new * dm.G + 15) / 16);
   const int64_t want = (dm.max_keys * tiles + 148 * 6 - 1) / (148 * 6);
   CacheSplit sp;
-  sp.keys = (int)std::min<int64_t>(std::max<int64_t>((want + 127) / 128 * 128, 256), 4096);
+  sp.keys = (int)std::min<int64_t>(std::max<int64_t>((want + 127) / 128 * 128, 256), 2048);
   sp.parts = std::max((dm.max_keys + sp.keys - 1) / sp.keys, 1);
   return sp;
 }
