@@ -366,8 +366,9 @@ HGA_API int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t
  * h / (Hq/Hkv)); hga_cache_write has put the new tokens' own keys there before.
  *   Q, O bf16 [n_tokens, Hq, d]      LSE fp32 [n_tokens, Hq] (natural log; optional, may be NULL)
  * A row that sees no key gets O = 0 and LSE = -inf.  Rows outside cu_q are left as they were.  Keys and values that a row does not
- * see have no influence on it, not even infinities or NaN.  Products are of bf16 numbers (the cache's are), sums in fp32, the
- * probabilities bf16; O is divided by the sum of the rounded ones.  Results do not depend on what else is in the batch, nor change from
+ * see have no influence on it, not even infinities or NaN.  Products are of bf16 numbers (the cache's are), sums in fp32; the
+ * probabilities are rounded to bf16 (over a quantised pool to fp16: off by 2^-11 of themselves, or 2^-31 of the row's largest).  Numbers of a
+ * quantised pool below 2^-118 count as zeros.  Results do not depend on what else is in the batch, nor change from
  * run to run, except that max_len, max_new and n_seq decide how the keys are shared out.
  * workspace: device scratch of at least hga_cache_workspace_bytes() bytes (16-byte aligned; may be NULL where that is 0); contents
  * are overwritten.  Calls that share a workspace must not overlap. */

@@ -6,14 +6,19 @@
 // the other, so that neither waits.  Both read the same K and V tiles, which pass through one ring in shared memory.
 //
 //   warps 0-3, 4-7   softmax and epilogue of M-tile 0 and 1
-//   warp 8           issues the GEMMs
-//   warps 9, 10      copy K and V tiles by TMA, a box per page part (bf16 pages)
-//   warps 12-15      quantised pages: fetch, convert to bf16 and store K and V tiles; bf16 pages: clean the last V tiles
+//   warps 8, 9       issue the GEMMs of M-tile 0 and 1
+//   warps 10, 11     copy K and V tiles by TMA, a box per page part (bf16 pages)
+//   warps 12-15      quantised pages: fetch, convert and store K and V tiles; bf16 pages: clean the last V tiles
+//
+// Quantised pages are multiplied as fp16, into which the converter instructions go and which holds e4m3 and e2m1 with their scales
+// exactly while these lie in a range of 2^22 (e4m3; Q is brought to fp16 by a power of two per row, exactly but for numbers 2^-29 of
+// the row's largest).  A unit that meets another scale starts again in bf16.
 //
 // A hidden key has weight zero, which does not silence a V row that is not finite.  So in the tiles that hold keys hidden from the
 // unit's first row (the last ones), numbers that are not finite are replaced by zeros, rows behind the last key altogether, and the
 // rows that do see such numbers get them added at the end.
 #include <algorithm>
+#include <type_traits>
 
 #include "hga_cache.cuh"
 #include "hga_sm100.cuh"
@@ -28,9 +33,9 @@ constexpr int kThreads = 512;
 constexpr int kTile = 128;                 // rows of an M-tile, keys of a tile
 constexpr uint32_t kTmemCols = 512;
 constexpr float kNoRef = -1e30f;           // reference of a row that has seen no key: 2^(-inf - it) = 0
-// A row's reference is raised, and O rescaled, when a logit exceeds it by this much (log2): weights stay below 2^8, and most tiles
-// leave O alone.
-constexpr float kSlack = 8.f;
+// A row's reference is raised, and O rescaled, when a logit exceeds it by kSlack (log2), to kLow below the row's largest: most tiles
+// leave O alone, and fp16 weights go down to 2^-31 of the reference's.
+constexpr float kLow = 6.f, kSlack = 14.f;
 
 template <int D>
 struct Smem {
@@ -40,9 +45,11 @@ struct Smem {
   uint8_t ring[kSlots][kTileBytes];        // K and V tiles in turn
   uint64_t full[kSlots], empty[kSlots];    // full: four arrivals, whoever fills the slot
   uint64_t dirty[kSlots];                  // a V tile has arrived that has to be cleaned before it is full
-  uint64_t s_full[2], p_full[2], o_full[2], drain;
+  uint64_t s_full[2], p_full[2][2], o_full[2], drain[2];      // p_full: a half of the tile's keys each
+  // (no member between the barriers)
+  float q_scale[2 * kTile];                // of a row's logits (fp16: the power of two taken out of Q, and the lift of K)
   uint32_t tmem_base;
-  int abort, strange;
+  int abort, strange, wide;                // wide: a scale outside fp16's range
   int seq, token0;                         // the unit's sequence, and its first token there
 };
 
@@ -62,6 +69,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // byte offset of 16-byte piece `c` of row r in a tile
 template <int D> __device__ __forceinline__ int piece(int r, int c) { return (c >> 3) * (kTile * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
 
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 __device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
   return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort));
 }
@@ -126,20 +143,24 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (bad) cache_status(status_word, HGA_STATUS_BAD_INDEX);
     if (lane == 0) { sm.seq = seq; sm.token0 = t0; }
   }
-  if (tid == 32) {
-    sm.abort = sm.strange = 0;
+  auto init_barriers = [&]() {
     for (int i = 0; i < NS; ++i) {
       mbar_init(&sm.full[i], 4);
-      mbar_init(&sm.empty[i], 1);
+      mbar_init(&sm.empty[i], 2);
       mbar_init(&sm.dirty[i], 1);
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(&sm.s_full[x], 1);
-      mbar_init(&sm.p_full[x], 4);
+      mbar_init(&sm.p_full[x][0], 4);
+      mbar_init(&sm.p_full[x][1], 4);
       mbar_init(&sm.o_full[x], 1);
+      mbar_init(&sm.drain[x], 1);
     }
-    mbar_init(&sm.drain, 1);
     fence_barrier_init();
+  };
+  if (tid == 32) {
+    sm.abort = sm.strange = sm.wide = 0;
+    init_barriers();
   }
   __syncthreads();
   const int seq = sm.seq, token0 = sm.token0;
@@ -167,15 +188,39 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
   // Q, rows that are none as zeros
   constexpr int C = D / 8;
-  for (int i = tid; i < 2 * kTile * C; i += kThreads) {
-    const int row = i / C, c = i % C, x = row / kTile, r = row % kTile;
-    const int t = dm.by_G(r), tok = x * plan.tokens + t;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (t < plan.tokens && tok < n_tok)
-      v = *reinterpret_cast<const uint4*>(Q + (s.q0 + token0 + tok) * dm.qs[0] + (h * dm.G + r - t * dm.G) * dm.qs[1] + c * 8);
-    *reinterpret_cast<uint4*>(sm.q[x] + piece<D>(r, c)) = v;
-  }
-  fence_proxy_async_smem();
+  constexpr bool kScaled = FMT != kCacheBf16;
+  // fp16: scales are 2^(code - 127 + kLift), in range from 2^-14 to 2^kTop
+  constexpr int kLift = FMT == kCacheMx8 ? 4 : 2, kTop = FMT == kCacheMx8 ? 7 : 13;
+  auto load_q = [&](bool f16) {
+    for (int i = tid; i < 2 * kTile * C; i += kThreads) {
+      const int row = i / C, c = i % C, x = row / kTile, r = row % kTile;
+      const int t = dm.by_G(r), tok = x * plan.tokens + t;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (t < plan.tokens && tok < n_tok)
+        v = *reinterpret_cast<const uint4*>(Q + (s.q0 + token0 + tok) * dm.qs[0] + (h * dm.G + r - t * dm.G) * dm.qs[1] + c * 8);
+      if (kScaled) {
+        float back = 1.f;
+        if (f16) {
+          // the row's largest to 2^14 .. 2^15, by a power of two that fp32 holds (and its inverse)
+          uint32_t* w = &v.x;
+          uint32_t big = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) big = max(big, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
+#pragma unroll
+          for (int k = 1; k < C; k <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, k));
+          const int up = max(min(127 + 14 - (int)(big >> 7), 100), -100);
+          const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+          back = __uint_as_float((uint32_t)(127 - up - kLift) << 23);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = pack_f16(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xffff0000u) * f);
+        }
+        if (c == 0) sm.q_scale[row] = back;
+      }
+      *reinterpret_cast<uint4*>(sm.q[x] + piece<D>(r, c)) = v;
+    }
+    fence_proxy_async_smem();
+  };
+  load_q(kScaled);
   if (warp == 8) {
     tmem_alloc(&sm.tmem_base, kTmemCols);
     tmem_relinquish();
@@ -186,6 +231,31 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   tc_fence_after_sync();
   if (tid == 0) pdl_launch_dependents();
   const uint32_t tmem = sm.tmem_base;
+  // Behind the last tile: every role is done, sm.abort, sm.strange and sm.wide are final.  True: once more, in bf16.
+  bool f16 = kScaled;
+  auto again = [&]() {
+    __syncwarp();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (!kScaled || !f16 || !sm.wide || *abort) return false;
+    f16 = false;
+    if (warp == 8 || warp == 9) {
+      // (the last commits may not have arrived yet)
+      mma_commit_w(elect_one(), &sm.drain[warp - 8]);
+      mbar_wait(&sm.drain[warp - 8], 0);
+    }
+    __syncwarp();
+    __syncthreads();
+    load_q(false);
+    if (tid == 0) {
+      sm.strange = 0;
+      for (uint64_t* b = sm.full; b < sm.drain + 2; ++b) mbar_inval(b);
+      init_barriers();
+    }
+    __syncthreads();
+    return true;
+  };
   // first tile with keys hidden from the unit's first row
   const int first_dirty = max(first_lim + 1 - k0, 0) / kTile;
 
@@ -201,10 +271,16 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const int tile_lim = min(pos0 + token0 + x * plan.tokens, s.keys - 1);       // of the M-tile's first row
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lanes + x * kTile, o_addr = tmem + lanes + 2 * kTile + x * D;
-    const float to_log2 = dm.scale * 1.44269504088896340736f;
-    const uint64_t to_log2_2 = pack_f32x2(to_log2, to_log2);
     float m = kNoRef, l = 0.f;
-    bool ok = true;
+    bool ok;
+    do {
+    const float to_log2 = dm.scale * 1.44269504088896340736f * (kScaled ? sm.q_scale[x * kTile + r] : 1.f);
+    const uint64_t to_log2_2 = pack_f32x2(to_log2, to_log2);
+    m = kNoRef;
+    l = 0.f;
+    ok = true;
+    auto tiles = [&](auto as_f16) {
+    constexpr bool kF16 = decltype(as_f16)::value;
 #pragma unroll 1
     for (int j = 0; j < n; ++j) {
       ok = all_wait(&sm.s_full[x], j & 1, abort);
@@ -223,16 +299,44 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
           for (int e = 0; e < 32; ++e)
             if (32 * i + e > seen) v[i][e] = 0xff800000u;
       }
-      float top[4];
+      // weights of half of the keys, stored over S's columns; returns their sum
+      auto weigh = [&](int half) {
+        const uint64_t neg_m = pack_f32x2(-m, -m);
+        uint64_t sum = pack_f32x2(0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        top[i] = __uint_as_float(v[i][0]);
+        for (int i = 2 * half; i < 2 * half + 2; ++i) {
+          uint32_t p[16];
 #pragma unroll
-        for (int e = 1; e < 32; ++e) top[i] = fmaxf(top[i], __uint_as_float(v[i][e]));
-      }
-      const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * to_log2;
-      if (__any_sync(0xffffffffu, mx > m + kSlack)) {
-        const float now = fmaxf(m, mx), f = fast_exp2(m - now);
+          for (int e = 0; e < 16; ++e) {
+            float a0, a1;
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i][2 * e]), __uint_as_float(v[i][2 * e + 1])), to_log2_2, neg_m), a0, a1);
+            a0 = fast_exp2(a0);
+            a1 = fast_exp2(a1);
+            sum = add_f32x2(sum, pack_f32x2(a0, a1));
+            p[e] = kF16 ? pack_f16(a0, a1) : pack_bf16(a0, a1);
+          }
+          tmem_st16(s_addr + 16 * i, p);
+        }
+        float s0, s1;
+        unpack_f32x2(sum, s0, s1);
+        return s0 + s1;
+      };
+      // The first half goes ahead with the reference at hand, while the tile's largest logit is looked for; where that is too large
+      // (in the first tile, and seldom after it) it is done again.
+      float sum;
+#pragma unroll 1
+      for (;;) {
+        sum = weigh(0);
+        float top[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          top[i] = __uint_as_float(v[i][0]);
+#pragma unroll
+          for (int e = 1; e < 32; ++e) top[i] = fmaxf(top[i], __uint_as_float(v[i][e]));
+        }
+        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * to_log2;
+        if (!__any_sync(0xffffffffu, mx > m + kSlack)) break;
+        const float now = fmaxf(m, mx - kLow), f = fast_exp2(m - now);
         m = now;
         l *= f;
         if (j > 0) {
@@ -247,37 +351,25 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
           }
         }
       }
-      const uint64_t neg_m = pack_f32x2(-m, -m);
-      uint64_t sum = pack_f32x2(0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t p[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float a0, a1;
-          unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i][2 * e]), __uint_as_float(v[i][2 * e + 1])), to_log2_2, neg_m), a0, a1);
-          a0 = fast_exp2(a0);
-          a1 = fast_exp2(a1);
-          sum = add_f32x2(sum, pack_f32x2(a0, a1));
-          p[e] = pack_bf16(a0, a1);
-        }
-        tmem_st16(s_addr + 16 * i, p);
-      }
-      float s0, s1;
-      unpack_f32x2(sum, s0, s1);
-      l += s0 + s1;
       tmem_wait_st();
       tc_fence_before_sync();
-      mbar_arrive_warp(&sm.p_full[x]);
+      mbar_arrive_warp(&sm.p_full[x][0]);
+      l += sum + weigh(1);
+      tmem_wait_st();
+      tc_fence_before_sync();
+      mbar_arrive_warp(&sm.p_full[x][1]);
     }
+    };
+    if (f16) tiles(std::true_type{});
+    else tiles(std::false_type{});
     if (ok && n > 0) ok = all_wait(&sm.o_full[x], 0, abort);
-    __syncwarp();
-    __syncthreads();                           // every role is done: sm.strange and sm.abort are final
+    } while (again());
     if (!*abort && n_tok > x * plan.tokens) {
       tc_fence_after_sync();
       const bool whole = s.keys <= plan.sp.keys;
       const int64_t all_rows = (int64_t)dm.n_tokens * dm.Hq, out_row = (int64_t)row * dm.Hq + head;
-      const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);                // (NaN stays NaN)
+      const float down = f16 ? 1.f / (float)(1 << kLift) : 1.f;                   // (V's lift)
+      const float inv = l > 0.f ? (whole ? 1.f / l : 1.f) * down : (l == 0.f ? 0.f : l);      // (NaN stays NaN)
 #pragma unroll 1
       for (int c = 0; c < D; c += 32) {
         uint32_t o[32];
@@ -318,7 +410,9 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         } else {
           uint4* dst = reinterpret_cast<uint4*>(part_o + (part * all_rows + out_row) * D + c);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          for (int e = 0; e < 8; ++e)
+            reinterpret_cast<float4*>(dst)[e] = make_float4(__uint_as_float(o[4 * e]) * inv, __uint_as_float(o[4 * e + 1]) * inv,
+                                                            __uint_as_float(o[4 * e + 2]) * inv, __uint_as_float(o[4 * e + 3]) * inv);
         }
       }
       if (real && whole && LSE) LSE[out_row] = l > 0.f ? (m + log2f(l)) * 0.69314718055994530942f : (l == 0.f ? -INFINITY : l);
@@ -327,28 +421,33 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (warp == 8) {
+    do {
+    if (warp < 10) {
       // ---------------------------------------------------------------- GEMMs (the whole warp stays together, one lane issues)
+      const int x = warp - 8, n = x ? n1 : n0;
       const uint32_t lead = elect_one();
-      constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTile, 0, 0), idesc_o = idesc_bf16_f32(128, D, 0, 1);
-      const uint64_t q_desc = smem_desc_sw128(smem_u32(sm.q), 16, 1024);
+      constexpr uint32_t kBf16 = (1u << 7) | (1u << 10);      // formats of A and B: bf16, else fp16
+      const uint32_t type = f16 ? kBf16 : 0;
+      const uint32_t idesc_s = idesc_bf16_f32(128, kTile, 0, 0) ^ type, idesc_o = idesc_bf16_f32(128, D, 0, 1) ^ type;
+      const uint64_t q_desc = smem_desc_sw128(smem_u32(sm.q[x]), 16, 1024);
       const uint64_t k_desc = smem_desc_sw128(smem_u32(sm.ring), 16, 1024), v_desc = smem_desc_sw128(smem_u32(sm.ring), kTile * 128, 1024);
-      auto issue_s = [&](int x, int slot) {
-        const uint64_t a = desc_advance(q_desc, x * Sm::kTileBytes), b = desc_advance(k_desc, slot * Sm::kTileBytes);
+      auto issue_s = [&](int slot) {
+        const uint64_t b = desc_advance(k_desc, slot * Sm::kTileBytes);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
           const uint32_t off = (i >> 2) * (kTile * 128) + (i & 3) * 32;
-          mma_ss_w(lead, tmem + x * kTile, desc_advance(a, off), desc_advance(b, off), idesc_s, i > 0);
+          mma_ss_w(lead, tmem + x * kTile, desc_advance(q_desc, off), desc_advance(b, off), idesc_s, i > 0);
         }
         mma_commit_w(lead, &sm.s_full[x]);
       };
-      auto issue_pv = [&](int x, int slot, bool add) {
-        const uint64_t b = desc_advance(v_desc, slot * Sm::kTileBytes);
+      auto issue_pv = [&](int half, int slot, bool add) {
+        const uint64_t b = desc_advance(v_desc, slot * Sm::kTileBytes + half * (kTile / 2 * 128));
 #pragma unroll
-        for (int i = 0; i < kTile / 16; ++i)
-          mma_ts_w(lead, tmem + 2 * kTile + x * D, tmem + x * kTile + 8 * i, desc_advance(b, i * 2048), idesc_o, add || i > 0);
+        for (int i = 0; i < kTile / 32; ++i)
+          mma_ts_w(lead, tmem + 2 * kTile + x * D, tmem + x * kTile + half * (kTile / 4) + 8 * i, desc_advance(b, i * 2048), idesc_o, add || i > 0);
       };
-      // position in the ring of K(j) is 2j, of V(j) 2j + 1
+      // Position in the ring of K(j) is 2j, of V(j) 2j + 1.  Both warps release every slot, whether its keys concern their M-tile or not,
+      // and always by a commit.
       int slot = 0;
       uint32_t phase = 0;
       auto next = [&]() { if (++slot == NS) { slot = 0; phase ^= 1; } };
@@ -357,40 +456,40 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         ok = all_wait(&sm.full[0], 0, abort);
         if (ok) {
           tc_fence_after_sync();
-          if (n0 > 0) issue_s(0, 0);
-          if (n1 > 0) issue_s(1, 0);
+          if (n > 0) issue_s(0);
           mma_commit_w(lead, &sm.empty[0]);
           next();
         }
       }
 #pragma unroll 1
       for (int j = 0; ok && j < n_tiles; ++j) {
-        const int v_slot = slot;
-        ok = all_wait(&sm.full[v_slot], phase, abort);
-        next();
-        const bool more = j + 1 < n_tiles;
-        if (ok && more) ok = all_wait(&sm.full[slot], phase, abort);
-#pragma unroll 1
-        for (int x = 0; ok && x < 2; ++x) {
-          const int n = x ? n1 : n0;
-          if (j >= n) continue;
-          ok = all_wait(&sm.p_full[x], j & 1, abort);
+        ok = all_wait(&sm.full[slot], phase, abort);
+        if (!ok) break;
+        if (j < n) {
+          ok = all_wait(&sm.p_full[x][0], j & 1, abort);
           if (!ok) break;
           tc_fence_after_sync();
-          issue_pv(x, v_slot, j > 0);
-          if (j + 1 < n) issue_s(x, slot);
-          else mma_commit_w(lead, &sm.o_full[x]);
+          issue_pv(0, slot, j > 0);
+          ok = all_wait(&sm.p_full[x][1], j & 1, abort);
+          if (!ok) break;
+          tc_fence_after_sync();
+          issue_pv(1, slot, true);
         }
-        if (!ok) break;
-        mma_commit_w(lead, &sm.empty[v_slot]);
-        if (more) {
+        mma_commit_w(lead, &sm.empty[slot]);
+        next();
+        if (j + 1 == n) mma_commit_w(lead, &sm.o_full[x]);
+        if (j + 1 < n_tiles) {
+          ok = all_wait(&sm.full[slot], phase, abort);
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (j + 1 < n) issue_s(slot);
           mma_commit_w(lead, &sm.empty[slot]);
           next();
         }
       }
-    } else if (FMT == kCacheBf16 && warp < 11) {
-      // ---------------------------------------------------------------- copies of K (warp 9) and V (warp 10)
-      const bool is_v = warp == 10;
+    } else if (FMT == kCacheBf16) {
+      // ---------------------------------------------------------------- copies of K (warp 10) and V (warp 11)
+      const bool is_v = warp == 11;
       const CUtensorMap* map = is_v ? &map_v : &map_k;
       const int boxes = kTile / plan.box, n_box = boxes * (D / 64);
       bool bad = false;
@@ -422,11 +521,11 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         for (int it = 0; it < 64; ++it) __nanosleep(1000);
       }
     }
-    __syncwarp();
-    __syncthreads();
+    } while (again());
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     const int w = warp - 12;
+    do {
     bool strange = false;
     if (FMT == kCacheBf16) {
       // ---------------------------------------------------------------- V tiles with hidden keys: a thread per key
@@ -467,7 +566,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const int in_row = lane % LPR;
       uint4 raw16[LPR];
       uint32_t code[LPR];
-      bool bad = false;
+      bool bad = false, wide = false;
       int page_next = 0, row_next = 0;                         // of key octet `lane` (0-15) of the tile after the one in flight
       auto look_up = [&](int j) {
         const int key = k0 + j * kTile + (lane & 15) * 8;
@@ -509,28 +608,39 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
           const int r = i * (4 * RPI) + w * RPI + lane / LPR;
           uint32_t sc = code[i];
           if (is_v && sc == 255 && k0 + j * kTile + r > first_lim) { sc = 0; strange = true; }
-          const uint32_t mul = pair(scale_bits(sc));
           const uint32_t q[4] = {raw16[i].x, raw16[i].y, raw16[i].z, raw16[i].w};
-          if (FMT == kCacheMx8) {
-            uint32_t o[8];
+          // pairs of neighbours: four of a word of e2m1, two of e4m3
+          constexpr int kPairs = FMT == kCacheMx8 ? 2 : 4;
+          uint32_t o[4 * kPairs];
+          if (f16) {
+            // (2^-127 counts as zero: so do numbers below 2^-118)
+            const uint32_t e = sc - (127 - kLift - 15);
+            const bool in = e - 1 < kTop + 15;
+            wide = wide || !(in || sc == 0 || sc == 255);
+            const uint32_t mul = pair(in ? e << 10 : sc == 255 ? 0x7e00u : 0u);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              o[2 * k] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x1404)), kTwo120), mul);
-              o[2 * k + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x3424)), kTwo120), mul);
-            }
+            for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-              *reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, 2 * in_row + k)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+              for (int y = 0; y < kPairs; ++y)
+                o[k * kPairs + y] = mul_f16x2(FMT == kCacheMx8 ? e4m3x2_to_f16(q[k] >> (16 * y)) : e2m1x2_to_f16(q[k] >> (8 * y)), mul);
           } else {
+            const uint32_t mul = pair(scale_bits(sc));
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              uint32_t o[4];
-              e2m1x4_to_bf16(q[k] & 0xffffu, o[0], o[1]);
-              e2m1x4_to_bf16(q[k] >> 16, o[2], o[3]);
-              *reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, 4 * in_row + k)) =
-                  make_uint4(mul_bf16x2(o[0], mul), mul_bf16x2(o[1], mul), mul_bf16x2(o[2], mul), mul_bf16x2(o[3], mul));
+              if (FMT == kCacheMx8) {
+                o[k * kPairs] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x1404)), kTwo120), mul);
+                o[k * kPairs + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x3424)), kTwo120), mul);
+              } else {
+                e2m1x4_to_bf16(q[k] & 0xffffu, o[k * kPairs], o[k * kPairs + 1]);
+                e2m1x4_to_bf16(q[k] >> 16, o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
+#pragma unroll
+                for (int y = 0; y < kPairs; ++y) o[k * kPairs + y] = mul_bf16x2(o[k * kPairs + y], mul);
+              }
             }
           }
+#pragma unroll
+          for (int k = 0; k < kPairs; ++k)
+            *reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, kPairs * in_row + k)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
         }
         fence_proxy_async_smem();
         mbar_arrive_warp(&sm.full[slot]);
@@ -540,10 +650,10 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
       }
       if (bad) cache_status(status_word, HGA_STATUS_BAD_INDEX);
+      if (wide) sm.wide = 1;
     }
     if (strange) sm.strange = 1;
-    __syncwarp();
-    __syncthreads();
+    } while (again());
   }
 
   // common exit
@@ -551,14 +661,14 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   tc_fence_before_sync();
   __syncthreads();
   if (tid == 0 && sm.abort && status_word) atomicOr(status_word, HGA_STATUS_WAIT_TIMEOUT);
-  if (warp == 8) {
+  if ((warp == 8 || warp == 9) && sm.abort) {
+    // given up: GEMMs already issued may still be writing tensor memory; wait (bounded) until the tensor pipe has run dry
+    mma_commit_w(elect_one(), &sm.drain[warp - 8]);
+    mbar_wait(&sm.drain[warp - 8], 0);
     __syncwarp();
-    if (sm.abort) {
-      // given up: GEMMs already issued may still be writing tensor memory; wait (bounded) until the tensor pipe has run dry
-      mma_commit_w(elect_one(), &sm.drain);
-      mbar_wait(&sm.drain, 0);
-      __syncwarp();
-    }
+  }
+  __syncthreads();
+  if (warp == 8) {
     tmem_dealloc(sm.tmem_base, kTmemCols);
   }
 }

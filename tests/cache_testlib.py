@@ -163,7 +163,9 @@ class Problem:
         most 2^-8 sum w |v - O| <= 2^-8 (sum w |v| + |O|); O's own rounding adds 2^-8 |O|.  A logit is a sum of d exact products
         in fp32, each addition off by 2^-23 of sum |q k| at most (the tensor pipe cuts off instead of rounding), and so is a sum of up to
         n weighted values; exp2 and the powers that join partial sums are off by 2^-21 together.  A weight below 2^-126 of the row's reference (which is
-        2^8 below its largest at most) is zero in fp32: with up to 2^20 keys and values below 2^6 that adds 2^-92 at most.  LSE: the logit's error, the sums'
+        2^14 below its largest at most) is zero in fp32: with up to 2^20 keys and values below 2^6 that adds 2^-92 at most.  Quantised pages:
+        weights are fp16, whose numbers below 2^-14 are 2^-24 apart, i.e. off by 2^-25; the row's largest is 2^6 or more in the same units, so
+        a weight is off by 2^-31 of the largest at most, and O by that times sum |v|.  LSE: the logit's error, the sums'
         and the logarithm's, and its own rounding."""
         q = f64(Q)
         scale = scale or 1 / np.sqrt(self.d)
@@ -190,6 +192,8 @@ class Problem:
                     off = (self.d + 4) * 2.0 ** -23 * size.max() + 2.0 ** -21
                     a = w @ np.abs(v)
                     tol_O[row, h] = 2.0 ** -8 * (a + 2 * np.abs(O[row, h])) + 2 * (off + 2.0 ** -23 * min(end, 4096)) * (a + np.abs(O[row, h])) + 2.0 ** -92
+                    if self.fmt != "bf16":
+                        tol_O[row, h] += 2.0 ** -31 * w.max() * np.abs(v).sum(0)
                     tol_L[row, h] = 2 * off + 2.0 ** -23 * min(end, 4096) + 2.0 ** -22 * np.abs(LSE[row, h])
         return O, LSE, tol_O, tol_L
 

@@ -306,6 +306,27 @@ def test_large_logits_in_any_order(fmt, seqs):
     pr.check_attn(Q, O, LSE)
 
 
+@pytest.mark.parametrize("fmt", ("mx8", "mx4"))
+@pytest.mark.parametrize("seqs,hq", (([(1, 300), (2, 90)], 4), ([(100, 300), (40, 40)], 4)))
+@pytest.mark.parametrize("which", ("K tiny", "V tiny", "V huge", "K huge", "V mixed", "all"))
+def test_scales_of_every_size(fmt, seqs, hq, which):
+    """quantised pages are multiplied as fp16 where their scales allow: here some or all do not"""
+    pr = T.Problem(seqs, fmt, hq=hq, hkv=2, d=64, seed=20)
+    up = {"K tiny": (-40, 0), "V tiny": (0, -60), "V huge": (0, 60), "K huge": (30, 0), "V mixed": (0, 0), "all": (-70, 40)}[which]
+    for name, by in zip("KV", up):
+        sc = getattr(pr, name + "_scale")
+        sc += by
+        if name == "V" and which == "V mixed":
+            sc[:, :, 3::5] += 30
+            sc[:, :, 4::7] -= 45
+    Q = pr.randn(pr.n_tokens, hq, 64)
+    Q = (Q.float() * 2.0 ** -up[0]).bfloat16()                               # logits of ordinary size
+    Q[1] *= 2.0 ** -20
+    O, LSE = pr.run_attn(Q.cuda())
+    pr.check_attn(Q, O, LSE)
+    assert int(pr.status.item()) == 0
+
+
 def test_scale_and_strides_of_q_and_o():
     pr = T.Problem([(3, 70), (80, 90)], "mx8", hq=4, hkv=2, d=128, seed=15)
     wide = pr.randn(pr.n_tokens, 3, 4, 128)
