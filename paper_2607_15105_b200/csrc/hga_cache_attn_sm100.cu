@@ -7,8 +7,11 @@
 //
 //   warps 0-3, 4-7   softmax and epilogue of M-tile 0 and 1
 //   warps 8, 9       issue the GEMMs of M-tile 0 and 1
-//   warps 10, 11     copy K and V tiles by TMA, a box per page part (bf16 pages)
-//   warps 12-15      quantised pages: fetch, convert and store K and V tiles; bf16 pages: clean the last V tiles
+//   warps 10, 11     copy K and V tiles by TMA, a box per page part (quantised pages: as they are, warp 10 alone)
+//   warps 12-15      quantised pages: convert K and V tiles; bf16 pages: clean the last V tiles
+//
+// The exponentials of the two M-tiles take turns as well (`turn`): left alone, both wait for the tensor pipe at one time and for the
+// special-function units at another.
 //
 // Quantised pages are multiplied as fp16, into which the converter instructions go and which holds e4m3 and e2m1 with their scales
 // exactly while these lie in a range of 2^22 (e4m3; Q is brought to fp16 by a power of two per row, exactly but for numbers 2^-29 of
@@ -37,21 +40,27 @@ constexpr float kNoRef = -1e30f;           // reference of a row that has seen n
 // leave O alone, and fp16 weights go down to 2^-31 of the reference's.
 constexpr float kLow = 6.f, kSlack = 14.f;
 
-template <int D>
+template <int FMT, int D>
 struct Smem {
-  static constexpr int kSlots = D == 128 ? 5 : 10;
+  static constexpr bool kScaled = FMT != kCacheBf16;
   static constexpr int kTileBytes = kTile * D * 2;
+  static constexpr int kSlots = (kScaled ? 4 : 5) * 128 / D;
+  static constexpr int kRaw = kScaled ? kTile * cache_row_bytes(FMT, D) : 0, kRawScales = kScaled ? kTile * (D / 32) : 0;
   uint8_t q[2][kTileBytes];                // [panel of 64 elements][row][128 bytes], 128-byte swizzle, as all tiles
   uint8_t ring[kSlots][kTileBytes];        // K and V tiles in turn
+  uint8_t raw[2][kScaled ? kRaw + kRawScales : 128];      // quantised tiles as they lie in their pages, rows one behind the other, and their scales
   uint64_t full[kSlots], empty[kSlots];    // full: four arrivals, whoever fills the slot
-  uint64_t dirty[kSlots];                  // a V tile has arrived that has to be cleaned before it is full
-  uint64_t s_full[2], p_full[2][2], o_full[2], drain[2];      // p_full: a half of the tile's keys each
+  uint64_t raw_full[kSlots];               // what has to be converted has arrived (two); a V tile that has to be cleaned (any slot)
+  uint64_t raw_empty[2];
+  uint64_t s_full[2], p_full[2][2], turn[2], o_full[2], drain[2];      // p_full: a half of the tile's keys each
   // (no member between the barriers)
-  float q_scale[2 * kTile];                // of a row's logits (fp16: the power of two taken out of Q, and the lift of K)
+  int8_t q_up[2 * kTile];                  // fp16: the power of two that a row of Q was multiplied by
   uint32_t tmem_base;
   int abort, strange, wide;                // wide: a scale outside fp16's range
   int seq, token0;                         // the unit's sequence, and its first token there
 };
+
+__device__ __align__(16) const uint8_t kNoScales[kTile * 4] = {};      // of keys that are none
 
 struct Plan {
   int tokens;                              // of an M-tile
@@ -96,12 +105,12 @@ struct Unit {
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(kThreads, 1)
-k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const CacheDims dm,
-                   const Plan plan, const uint16_t* __restrict__ Q, const int32_t* __restrict__ cu_q,
+k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                   const CacheDims dm, const Plan plan, const uint16_t* __restrict__ Q, const int32_t* __restrict__ cu_q,
                    const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table, const uint8_t* __restrict__ K,
                    const uint8_t* __restrict__ V, const uint8_t* __restrict__ K_scale, const uint8_t* __restrict__ V_scale,
                    uint16_t* __restrict__ O, float* __restrict__ LSE, float* __restrict__ part_o, int32_t* status_word) {
-  typedef Smem<D> Sm;
+  typedef Smem<FMT, D> Sm;
   constexpr int NS = Sm::kSlots;
   extern __shared__ uint8_t raw[];
   Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -147,9 +156,11 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     for (int i = 0; i < NS; ++i) {
       mbar_init(&sm.full[i], 4);
       mbar_init(&sm.empty[i], 2);
-      mbar_init(&sm.dirty[i], 1);
+      mbar_init(&sm.raw_full[i], 1);
     }
     for (int x = 0; x < 2; ++x) {
+      mbar_init(&sm.raw_empty[x], 4);
+      mbar_init(&sm.turn[x], 4);
       mbar_init(&sm.s_full[x], 1);
       mbar_init(&sm.p_full[x][0], 4);
       mbar_init(&sm.p_full[x][1], 4);
@@ -199,7 +210,6 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       if (t < plan.tokens && tok < n_tok)
         v = *reinterpret_cast<const uint4*>(Q + (s.q0 + token0 + tok) * dm.qs[0] + (h * dm.G + r - t * dm.G) * dm.qs[1] + c * 8);
       if (kScaled) {
-        float back = 1.f;
         if (f16) {
           // the row's largest to 2^14 .. 2^15, by a power of two that fp32 holds (and its inverse)
           uint32_t* w = &v.x;
@@ -210,11 +220,10 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
           for (int k = 1; k < C; k <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, k));
           const int up = max(min(127 + 14 - (int)(big >> 7), 100), -100);
           const float f = __uint_as_float((uint32_t)(127 + up) << 23);
-          back = __uint_as_float((uint32_t)(127 - up - kLift) << 23);
+          if (c == 0) sm.q_up[row] = (int8_t)up;
 #pragma unroll
           for (int k = 0; k < 4; ++k) w[k] = pack_f16(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xffff0000u) * f);
         }
-        if (c == 0) sm.q_scale[row] = back;
       }
       *reinterpret_cast<uint4*>(sm.q[x] + piece<D>(r, c)) = v;
     }
@@ -274,7 +283,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     float m = kNoRef, l = 0.f;
     bool ok;
     do {
-    const float to_log2 = dm.scale * 1.44269504088896340736f * (kScaled ? sm.q_scale[x * kTile + r] : 1.f);
+    const float to_log2 = dm.scale * 1.44269504088896340736f * (kScaled && f16 ? __uint_as_float((uint32_t)(127 - sm.q_up[x * kTile + r] - kLift) << 23) : 1.f);
     const uint64_t to_log2_2 = pack_f32x2(to_log2, to_log2);
     m = kNoRef;
     l = 0.f;
@@ -298,6 +307,10 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             if (32 * i + e > seen) v[i][e] = 0xff800000u;
+      }
+      if (x == 0 ? j > 0 && j <= n1 : j < n0) {
+        ok = all_wait(&sm.turn[x], (x == 0 ? j - 1 : j) & 1, abort);
+        if (!ok) break;
       }
       // weights of half of the keys, stored over S's columns; returns their sum
       auto weigh = [&](int half) {
@@ -355,6 +368,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       tc_fence_before_sync();
       mbar_arrive_warp(&sm.p_full[x][0]);
       l += sum + weigh(1);
+      mbar_arrive_warp(&sm.turn[x ^ 1]);
       tmem_wait_st();
       tc_fence_before_sync();
       mbar_arrive_warp(&sm.p_full[x][1]);
@@ -463,57 +477,83 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
 #pragma unroll 1
       for (int j = 0; ok && j < n_tiles; ++j) {
-        ok = all_wait(&sm.full[slot], phase, abort);
-        if (!ok) break;
-        if (j < n) {
+        // V(j), and K(j + 1) ahead of the second half of P(j), whose arrival the softmax threads' next S hangs on
+        const int v_slot = slot;
+        const bool more = j + 1 < n_tiles;
+        ok = all_wait(&sm.full[v_slot], phase, abort);
+        next();
+        const int k_slot = slot;
+        if (ok && j < n) {
           ok = all_wait(&sm.p_full[x][0], j & 1, abort);
           if (!ok) break;
           tc_fence_after_sync();
-          issue_pv(0, slot, j > 0);
-          ok = all_wait(&sm.p_full[x][1], j & 1, abort);
-          if (!ok) break;
-          tc_fence_after_sync();
-          issue_pv(1, slot, true);
+          issue_pv(0, v_slot, j > 0);
         }
-        mma_commit_w(lead, &sm.empty[slot]);
-        next();
+        if (ok && more) ok = all_wait(&sm.full[k_slot], phase, abort);
+        if (ok && j < n) ok = all_wait(&sm.p_full[x][1], j & 1, abort);
+        if (!ok) break;
+        tc_fence_after_sync();
+        if (j < n) issue_pv(1, v_slot, true);
+        if (j + 1 < n) issue_s(k_slot);
+        mma_commit_w(lead, &sm.empty[v_slot]);
         if (j + 1 == n) mma_commit_w(lead, &sm.o_full[x]);
-        if (j + 1 < n_tiles) {
-          ok = all_wait(&sm.full[slot], phase, abort);
-          if (!ok) break;
-          tc_fence_after_sync();
-          if (j + 1 < n) issue_s(slot);
-          mma_commit_w(lead, &sm.empty[slot]);
+        if (more) {
+          mma_commit_w(lead, &sm.empty[k_slot]);
           next();
         }
       }
-    } else if (FMT == kCacheBf16) {
-      // ---------------------------------------------------------------- copies of K (warp 10) and V (warp 11)
-      const bool is_v = warp == 11;
-      const CUtensorMap* map = is_v ? &map_v : &map_k;
-      const int boxes = kTile / plan.box, n_box = boxes * (D / 64);
+    } else if (!kScaled || warp == 10) {
+      // ---------------------------------------------------------------- copies: of K by warp 10, of V by warp 11; quantised: both by 10
+      const int boxes = kTile / plan.box;
       bool bad = false;
+      // lane's box `at` of tile j: its page (a page behind the last one arrives as zeros) and row there
+      auto place = [&](int j, int at, int& r) {
+        const int key = k0 + j * kTile + at * plan.box;
+        r = 0;
+        if (key >= k1) return dm.n_pages;
+        const int e = dm.by_page(key), page = table[seq * dm.table_stride + e];
+        if (page < 0 || page >= dm.n_pages) { bad = true; return dm.n_pages; }
+        r = key - e * dm.page;
+        return page;
+      };
+      if (!kScaled) {
+        const bool is_v = warp == 11;
+        const CUtensorMap* map = is_v ? &map_v : &map_k;
 #pragma unroll 1
-      for (int j = 0; j < n_tiles; ++j) {
-        const int at_ring = 2 * j + is_v, use = at_ring / NS, slot = at_ring - use * NS;
-        if (!all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
-        uint64_t* bar = is_v && j >= first_dirty ? &sm.dirty[slot] : &sm.full[slot];
-        if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kTileBytes);
-        else if (lane < 4 && bar == &sm.full[slot]) mbar_arrive(bar);
-        __syncwarp();
-        if (lane < n_box) {
-          const int box = lane % boxes, panel = lane / boxes;
-          const int key = k0 + j * kTile + box * plan.box;
-          int page = dm.n_pages, r = 0;        // (a page behind the last one arrives as zeros)
-          if (key < k1) {
-            const int e = dm.by_page(key);
-            r = key - e * dm.page;
-            page = table[seq * dm.table_stride + e];
-            if (page < 0 || page >= dm.n_pages) { bad = true; page = dm.n_pages; }
+        for (int j = 0; j < n_tiles; ++j) {
+          const int at_ring = 2 * j + is_v, use = at_ring / NS, slot = at_ring - use * NS;
+          if (!all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
+          uint64_t* bar = is_v && j >= first_dirty ? &sm.raw_full[slot] : &sm.full[slot];
+          if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kTileBytes);
+          else if (lane < 4 && bar == &sm.full[slot]) mbar_arrive(bar);
+          __syncwarp();
+          if (lane < boxes * (D / 64)) {
+            const int box = lane % boxes, panel = lane / boxes;
+            int r;
+            const int page = place(j, box, r);
+            tma_load_5d(sm.ring[slot] + panel * (kTile * 128) + box * plan.box * 128, map, bar, 0, r, panel, h, page);
           }
-          tma_load_5d(sm.ring[slot] + panel * (kTile * 128) + box * plan.box * 128, map, bar, 0, r, panel, h, page);
+          __syncwarp();
         }
-        __syncwarp();
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < 2 * n_tiles; ++i) {
+          const int j = i >> 1;
+          const bool is_v = i & 1;
+          uint8_t* dst = sm.raw[i & 1];
+          uint64_t* bar = &sm.raw_full[i & 1];
+          if (!all_wait(&sm.raw_empty[i & 1], ((i >> 1) & 1) ^ 1, abort)) break;
+          if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kRaw + Sm::kRawScales);
+          __syncwarp();
+          if (lane < boxes) {
+            int r;
+            const int page = place(j, lane, r);
+            tma_load_5d(dst + lane * plan.box * cache_row_bytes(FMT, D), is_v ? &map_v : &map_k, bar, 0, r, h, page, 0);
+            const uint8_t* scales = (is_v ? V_scale : K_scale) + (((int64_t)page * dm.Hkv + h) * dm.page + r) * (D / 32);
+            bulk_load(dst + Sm::kRaw + lane * plan.box * (D / 32), page < dm.n_pages ? scales : kNoScales, plan.box * (D / 32), bar);
+          }
+          __syncwarp();
+        }
       }
       if (bad) cache_status(status_word, HGA_STATUS_BAD_INDEX);
       if (*abort && lane == 0) {
@@ -530,11 +570,11 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (FMT == kCacheBf16) {
       // ---------------------------------------------------------------- V tiles with hidden keys: a thread per key
       const int r = tid & 127;
-      uint32_t parity = 0;                     // of each slot's `dirty`
+      uint32_t parity = 0;                     // of each slot's raw_full
 #pragma unroll 1
       for (int j = first_dirty; j < n_tiles; ++j) {
         const int slot = (2 * j + 1) % NS;
-        if (!all_wait(&sm.dirty[slot], (parity >> slot) & 1, abort)) break;
+        if (!all_wait(&sm.raw_full[slot], (parity >> slot) & 1, abort)) break;
         parity ^= 1u << slot;
         const int key = k0 + j * kTile + r;
         if (key > first_lim) {
@@ -560,55 +600,29 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         mbar_arrive_warp(&sm.full[slot]);
       }
     } else {
-      // ---------------------------------------------------------------- quantised pages: fetched a tile ahead, converted, stored
+      // ---------------------------------------------------------------- quantised tiles: converted from one buffer into another
       constexpr int LPR = cache_row_bytes(FMT, D) / 16;        // lanes of a row, and 16-byte pieces that a thread has of a tile
-      constexpr int RPI = 32 / LPR;                            // rows of one load instruction
+      constexpr int RPI = 32 / LPR;                            // rows of a warp's access
       const int in_row = lane % LPR;
-      uint4 raw16[LPR];
-      uint32_t code[LPR];
-      bool bad = false, wide = false;
-      int page_next = 0, row_next = 0;                         // of key octet `lane` (0-15) of the tile after the one in flight
-      auto look_up = [&](int j) {
-        const int key = k0 + j * kTile + (lane & 15) * 8;
-        page_next = -1;
-        if (key < k1) {
-          const int e = dm.by_page(key);
-          row_next = key - e * dm.page;
-          page_next = table[seq * dm.table_stride + e];
-          if (page_next < 0 || page_next >= dm.n_pages) { bad = true; page_next = -1; }
-        }
-      };
-      auto fetch = [&](int j, bool is_v) {
-        const uint8_t* src = is_v ? V : K;
-        const uint8_t* scales = is_v ? V_scale : K_scale;
-        const int64_t st0 = is_v ? dm.vs[0] : dm.ks[0], st1 = is_v ? dm.vs[1] : dm.ks[1], st2 = is_v ? dm.vs[2] : dm.ks[2];
-#pragma unroll
-        for (int i = 0; i < LPR; ++i) {
-          const int r = i * (4 * RPI) + w * RPI + lane / LPR, key = k0 + j * kTile + r;
-          const int page = __shfl_sync(0xffffffffu, page_next, r >> 3), pr = __shfl_sync(0xffffffffu, row_next, r >> 3) + (r & 7);
-          raw16[i] = make_uint4(0, 0, 0, 0);
-          code[i] = 127;
-          if (key < k1 && page >= 0) {
-            raw16[i] = __ldg(reinterpret_cast<const uint4*>(src + page * st0 + h * st1 + pr * st2 + in_row * 16));
-            code[i] = __ldg(scales + (((int64_t)page * dm.Hkv + h) * dm.page + pr) * (D / 32) + (FMT == kCacheMx8 ? in_row >> 1 : in_row));
-          }
-        }
-      };
-      if (n_tiles > 0) {
-        look_up(0);
-        fetch(0, false);
-      }
+      bool wide = false;
 #pragma unroll 1
       for (int i_ring = 0; i_ring < 2 * n_tiles; ++i_ring) {
         const int use = i_ring / NS, slot = i_ring - use * NS, j = i_ring >> 1;
         const bool is_v = i_ring & 1;
-        if (!all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
-#pragma unroll
+        if (!all_wait(&sm.raw_full[i_ring & 1], (i_ring >> 1) & 1, abort) || !all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
+        const uint8_t* src = sm.raw[i_ring & 1];
+        const int end = k1 - (k0 + j * kTile), hidden = is_v ? first_lim - (k0 + j * kTile) : kTile;      // rows from `end` on are none
+#pragma unroll 4
         for (int i = 0; i < LPR; ++i) {
           const int r = i * (4 * RPI) + w * RPI + lane / LPR;
-          uint32_t sc = code[i];
-          if (is_v && sc == 255 && k0 + j * kTile + r > first_lim) { sc = 0; strange = true; }
-          const uint32_t q[4] = {raw16[i].x, raw16[i].y, raw16[i].z, raw16[i].w};
+          uint4 y = *reinterpret_cast<const uint4*>(src + r * cache_row_bytes(FMT, D) + in_row * 16);
+          uint32_t sc = src[Sm::kRaw + r * (D / 32) + (FMT == kCacheMx8 ? in_row >> 1 : in_row)];
+          if (r >= end) {
+            y = make_uint4(0, 0, 0, 0);
+            sc = 0;
+          }
+          if (sc == 255 && r > hidden) { sc = 0; strange = true; }
+          const uint32_t q[4] = {y.x, y.y, y.z, y.w};
           // pairs of neighbours: four of a word of e2m1, two of e4m3
           constexpr int kPairs = FMT == kCacheMx8 ? 2 : 4;
           uint32_t o[4 * kPairs];
@@ -644,12 +658,8 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
         fence_proxy_async_smem();
         mbar_arrive_warp(&sm.full[slot]);
-        if (i_ring + 1 < 2 * n_tiles) {
-          if (is_v) look_up(j + 1);
-          fetch(is_v ? j + 1 : j, !is_v);
-        }
+        mbar_arrive_warp(&sm.raw_empty[i_ring & 1]);
       }
-      if (bad) cache_status(status_word, HGA_STATUS_BAD_INDEX);
       if (wide) sm.wide = 1;
     }
     if (strange) sm.strange = 1;
@@ -698,17 +708,25 @@ int launch_of(const CacheDims& dm, const Plan& plan, const void* Q, const int32_
   const int64_t ctas = (int64_t)plan.units * dm.Hkv * plan.sp.parts;
   if (ctas > 0x7fffffff) return HGA_ERR_SHAPE;
   CUtensorMap mk = {}, mv = {};
+  int bad;
   if (FMT == kCacheBf16) {
     const uint32_t box[5] = {64, (uint32_t)plan.box, 1, 1, 1};
     const uint64_t dims[5] = {64, (uint64_t)dm.page, (uint64_t)(D / 64), (uint64_t)dm.Hkv, (uint64_t)dm.n_pages};
     const uint64_t sk[4] = {(uint64_t)dm.ks[2] * 2, 128, (uint64_t)dm.ks[1] * 2, (uint64_t)dm.ks[0] * 2};
     const uint64_t sv[4] = {(uint64_t)dm.vs[2] * 2, 128, (uint64_t)dm.vs[1] * 2, (uint64_t)dm.vs[0] * 2};
-    if (encode_tensor_map_bf16(&mk, K, 5, dims, sk, box, true, false) || encode_tensor_map_bf16(&mv, V, 5, dims, sv, box, true, false))
-      return HGA_ERR_UNSUPPORTED;
+    bad = encode_tensor_map_bf16(&mk, K, 5, dims, sk, box, true, false) | encode_tensor_map_bf16(&mv, V, 5, dims, sv, box, true, false);
+  } else {
+    constexpr uint32_t kRow = cache_row_bytes(FMT, D);
+    const uint32_t box[5] = {kRow, (uint32_t)plan.box, 1, 1, 1};
+    const uint64_t dims[5] = {kRow, (uint64_t)dm.page, (uint64_t)dm.Hkv, (uint64_t)dm.n_pages, 1};
+    const uint64_t sk[4] = {(uint64_t)dm.ks[2], (uint64_t)dm.ks[1], (uint64_t)dm.ks[0], 16};
+    const uint64_t sv[4] = {(uint64_t)dm.vs[2], (uint64_t)dm.vs[1], (uint64_t)dm.vs[0], 16};
+    bad = encode_tensor_map_u8(&mk, K, 5, dims, sk, box) | encode_tensor_map_u8(&mv, V, 5, dims, sv, box);
   }
+  if (bad) return HGA_ERR_UNSUPPORTED;
   auto* kernel = k_cache_attn_sm100<FMT, D>;
-  const size_t smem = sizeof(Smem<D>) + 1024;
-  static_assert(sizeof(Smem<D>) + 1024 <= 232448, "shared memory of a CTA");
+  const size_t smem = sizeof(Smem<FMT, D>) + 1024;
+  static_assert(sizeof(Smem<FMT, D>) + 1024 <= 232448, "shared memory of a CTA");
   const int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem, true);
   if (rc) return rc;
   PdlLaunch cfg(dim3((unsigned)ctas), kThreads, smem, st, 0);

@@ -171,6 +171,12 @@ __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk
 // global writes may still be in flight: enough before the source is reused or the CTA exits)
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
+// Untiled bulk copy global -> shared (both addresses 16-byte aligned, bytes a multiple of 16), counted in bytes on `bar`.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
 // Untiled bulk copy shared -> global of `bytes` contiguous bytes (both addresses 16-byte aligned, bytes
 // a multiple of 16), bulk-group completion; the second form adds fp32 values into global memory.
 __device__ __forceinline__ void bulk_store(void* dst, uint32_t src_smem, uint32_t bytes) {
@@ -394,5 +400,8 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
 // to, those of earlier calls.
 int encode_tensor_map_bf16(CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
                            const uint64_t* strides_bytes, const uint32_t* box, bool swizzle128, bool keep = true);
+// ... of bytes, without a swizzle, not kept
+int encode_tensor_map_u8(CUtensorMap* out, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                         const uint32_t* box);
 
 }  // namespace hga
