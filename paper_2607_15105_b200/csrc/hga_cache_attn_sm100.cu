@@ -1,17 +1,16 @@
 // hga_cache_attn for chunks of new tokens (tcgen05 / TMEM / TMA).
 //
 // A unit is up to 256 query rows of one (sequence, key/value head) -- new tokens x query heads of the group, token by token -- as two
-// M-tiles of 128 rows, whose keys are taken in tiles of 128: S = Q K^T, P = 2^(S c - m), O += P V, with S, P and O in tensor memory.
-// The M-tiles take turns: while the softmax threads of one (four warps, a thread per row) work on S, the tensor pipe multiplies for
-// the other, so that neither waits.  Both read the same K and V tiles, which pass through one ring in shared memory.
+// M-tiles of 128 rows.  Keys come in tiles of 128, which both M-tiles read from one ring in shared memory, and are taken 64 at a time:
+// S = Q K^T, P = 2^(S c - m), O += P V, with S, P and O in tensor memory.  An M-tile has two buffers of 64 columns for S, over which
+// P is written: while its softmax threads (four warps, a thread per row) work on one, the tensor pipe fills the other, so they find
+// the next S ready.  (Steps of 128 keys with one buffer per M-tile, the M-tiles taking turns: 4200 cycles for 2 x 128 x 128, most of them
+// waiting for one another.)  Of S's GEMMs, N = 64 costs 1.5 times the cycles per key of N = 128: they are bound by reading Q.
 //
 //   warps 0-3, 4-7   softmax and epilogue of M-tile 0 and 1
 //   warps 8, 9       issue the GEMMs of M-tile 0 and 1
 //   warps 10, 11     copy K and V tiles by TMA, a box per page part (quantised pages: as they are, warp 10 alone)
 //   warps 12-15      quantised pages: convert K and V tiles; bf16 pages: clean the last V tiles
-//
-// The exponentials of the two M-tiles take turns as well (`turn`): left alone, both wait for the tensor pipe at one time and for the
-// special-function units at another.
 //
 // Quantised pages are multiplied as fp16, into which the converter instructions go and which holds e4m3 and e2m1 with their scales
 // exactly while these lie in a range of 2^22 (e4m3; Q is brought to fp16 by a power of two per row, exactly but for numbers 2^-29 of
@@ -34,6 +33,7 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kTile = 128;                 // rows of an M-tile, keys of a tile
+constexpr int kStep = 64;                  // keys of a step
 constexpr uint32_t kTmemCols = 512;
 constexpr float kNoRef = -1e30f;           // reference of a row that has seen no key: 2^(-inf - it) = 0
 // A row's reference is raised, and O rescaled, when a logit exceeds it by kSlack (log2), to kLow below the row's largest: most tiles
@@ -52,7 +52,9 @@ struct Smem {
   uint64_t full[kSlots], empty[kSlots];    // full: four arrivals, whoever fills the slot
   uint64_t raw_full[kSlots];               // what has to be converted has arrived (two); a V tile that has to be cleaned (any slot)
   uint64_t raw_empty[2];
-  uint64_t s_full[2], p_full[2][2], turn[2], o_full[2], drain[2];      // p_full: a half of the tile's keys each
+  // s_full, p_full: of M-tile x's buffer b.  s_full for the t-th time: S of step 2 t + b is there, if there is such a step, and P V of
+  // step 2 t + b - 2 done.
+  uint64_t s_full[2][2], p_full[2][2], drain[2];
   // (no member between the barriers)
   int8_t q_up[2 * kTile];                  // fp16: the power of two that a row of Q was multiplied by
   uint32_t tmem_base;
@@ -160,11 +162,10 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(&sm.raw_empty[x], 4);
-      mbar_init(&sm.turn[x], 4);
-      mbar_init(&sm.s_full[x], 1);
-      mbar_init(&sm.p_full[x][0], 4);
-      mbar_init(&sm.p_full[x][1], 4);
-      mbar_init(&sm.o_full[x], 1);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&sm.s_full[x][b], 1);
+        mbar_init(&sm.p_full[x][b], 4);
+      }
       mbar_init(&sm.drain[x], 1);
     }
     fence_barrier_init();
@@ -188,14 +189,14 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     pdl_launch_dependents();
     return;
   }
-  // tiles of each M-tile (the first one's rows see fewer keys)
-  auto tiles_of = [&](int x) {
+  // steps of each M-tile (the first one's rows see fewer keys)
+  auto steps_of = [&](int x) {
     const int n = min(n_tok - x * plan.tokens, plan.tokens);
     if (n <= 0) return 0;
     const int end = min(k1, min(pos0 + token0 + x * plan.tokens + n - 1, s.keys - 1) + 1);
-    return max(end - k0 + kTile - 1, 0) / kTile;
+    return max(end - k0 + kStep - 1, 0) / kStep;
   };
-  const int n0 = tiles_of(0), n1 = tiles_of(1), n_tiles = max(n0, n1);
+  const int n0 = steps_of(0), n1 = steps_of(1), n_tiles = (max(n0, n1) + 1) / 2;
 
   // Q, rows that are none as zeros
   constexpr int C = D / 8;
@@ -288,71 +289,66 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     m = kNoRef;
     l = 0.f;
     ok = true;
-    auto tiles = [&](auto as_f16) {
+    auto steps = [&](auto as_f16) {
     constexpr bool kF16 = decltype(as_f16)::value;
 #pragma unroll 1
     for (int j = 0; j < n; ++j) {
-      ok = all_wait(&sm.s_full[x], j & 1, abort);
+      ok = all_wait(&sm.s_full[x][j & 1], (j >> 1) & 1, abort);
       if (!ok) break;
       tc_fence_after_sync();
-      uint32_t v[4][32];
+      const uint32_t buf = s_addr + (j & 1) * kStep;
+      uint32_t v[2][32];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_ld32(s_addr + 32 * i, v[i]);
+      for (int i = 0; i < 2; ++i) tmem_ld32(buf + 32 * i, v[i]);
       tmem_wait_ld();
-      const int base = k0 + j * kTile;
-      if (base + kTile - 1 > tile_lim) {
+      const int base = k0 + j * kStep;
+      if (base + kStep - 1 > tile_lim) {
         const int seen = lim - base;           // columns up to it are visible
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             if (32 * i + e > seen) v[i][e] = 0xff800000u;
       }
-      if (x == 0 ? j > 0 && j <= n1 : j < n0) {
-        ok = all_wait(&sm.turn[x], (x == 0 ? j - 1 : j) & 1, abort);
-        if (!ok) break;
-      }
-      // weights of half of the keys, stored over S's columns; returns their sum
-      auto weigh = [&](int half) {
-        const uint64_t neg_m = pack_f32x2(-m, -m);
-        uint64_t sum = pack_f32x2(0.f, 0.f);
-#pragma unroll
-        for (int i = 2 * half; i < 2 * half + 2; ++i) {
-          uint32_t p[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float a0, a1;
-            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i][2 * e]), __uint_as_float(v[i][2 * e + 1])), to_log2_2, neg_m), a0, a1);
-            a0 = fast_exp2(a0);
-            a1 = fast_exp2(a1);
-            sum = add_f32x2(sum, pack_f32x2(a0, a1));
-            p[e] = kF16 ? pack_f16(a0, a1) : pack_bf16(a0, a1);
-          }
-          tmem_st16(s_addr + 16 * i, p);
-        }
-        float s0, s1;
-        unpack_f32x2(sum, s0, s1);
-        return s0 + s1;
-      };
-      // The first half goes ahead with the reference at hand, while the tile's largest logit is looked for; where that is too large
-      // (in the first tile, and seldom after it) it is done again.
+      // The weights are computed with the reference at hand, while the row's largest logit is looked for; where that is too large (in the
+      // first step, and seldom after it) they are computed again.
       float sum;
 #pragma unroll 1
       for (;;) {
-        sum = weigh(0);
-        float top[4];
+        const uint64_t neg_m = pack_f32x2(-m, -m);
+        uint64_t sum2[2];
+        float top[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2; ++i) {
+          uint32_t p[16];
+          sum2[i] = pack_f32x2(0.f, 0.f);
           top[i] = __uint_as_float(v[i][0]);
 #pragma unroll
-          for (int e = 1; e < 32; ++e) top[i] = fmaxf(top[i], __uint_as_float(v[i][e]));
+          for (int e = 0; e < 16; ++e) {
+            const float x0 = __uint_as_float(v[i][2 * e]), x1 = __uint_as_float(v[i][2 * e + 1]);
+            top[i] = fmaxf(top[i], fmaxf(x0, x1));
+            float a0, a1;
+            unpack_f32x2(fma_f32x2(pack_f32x2(x0, x1), to_log2_2, neg_m), a0, a1);
+            a0 = fast_exp2(a0);
+            a1 = fast_exp2(a1);
+            sum2[i] = add_f32x2(sum2[i], pack_f32x2(a0, a1));
+            p[e] = kF16 ? pack_f16(a0, a1) : pack_bf16(a0, a1);
+          }
+          tmem_st16(buf + 16 * i, p);
         }
-        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * to_log2;
+        float s0, s1;
+        unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
+        sum = s0 + s1;
+        const float mx = fmaxf(top[0], top[1]) * to_log2;
         if (!__any_sync(0xffffffffu, mx > m + kSlack)) break;
         const float now = fmaxf(m, mx - kLow), f = fast_exp2(m - now);
         m = now;
         l *= f;
         if (j > 0) {
+          // O may be touched when P V of the step before is done
+          ok = all_wait(&sm.s_full[x][(j + 1) & 1], ((j + 1) >> 1) & 1, abort);
+          if (!ok) break;
+          tc_fence_after_sync();
 #pragma unroll 1
           for (int c = 0; c < D; c += 16) {
             uint32_t o[16];
@@ -364,19 +360,16 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
           }
         }
       }
+      if (!ok) break;
+      l += sum;
       tmem_wait_st();
       tc_fence_before_sync();
-      mbar_arrive_warp(&sm.p_full[x][0]);
-      l += sum + weigh(1);
-      mbar_arrive_warp(&sm.turn[x ^ 1]);
-      tmem_wait_st();
-      tc_fence_before_sync();
-      mbar_arrive_warp(&sm.p_full[x][1]);
+      mbar_arrive_warp(&sm.p_full[x][j & 1]);
     }
     };
-    if (f16) tiles(std::true_type{});
-    else tiles(std::false_type{});
-    if (ok && n > 0) ok = all_wait(&sm.o_full[x], 0, abort);
+    if (f16) steps(std::true_type{});
+    else steps(std::false_type{});
+    if (ok && n > 0) ok = all_wait(&sm.s_full[x][(n + 1) & 1], ((n + 1) >> 1) & 1, abort);      // P V of the last step
     } while (again());
     if (!*abort && n_tok > x * plan.tokens) {
       tc_fence_after_sync();
@@ -442,23 +435,23 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const uint32_t lead = elect_one();
       constexpr uint32_t kBf16 = (1u << 7) | (1u << 10);      // formats of A and B: bf16, else fp16
       const uint32_t type = f16 ? kBf16 : 0;
-      const uint32_t idesc_s = idesc_bf16_f32(128, kTile, 0, 0) ^ type, idesc_o = idesc_bf16_f32(128, D, 0, 1) ^ type;
+      const uint32_t idesc_s = idesc_bf16_f32(128, kStep, 0, 0) ^ type, idesc_o = idesc_bf16_f32(128, D, 0, 1) ^ type;
       const uint64_t q_desc = smem_desc_sw128(smem_u32(sm.q[x]), 16, 1024);
       const uint64_t k_desc = smem_desc_sw128(smem_u32(sm.ring), 16, 1024), v_desc = smem_desc_sw128(smem_u32(sm.ring), kTile * 128, 1024);
-      auto issue_s = [&](int slot) {
-        const uint64_t b = desc_advance(k_desc, slot * Sm::kTileBytes);
+      const uint32_t s_tmem = tmem + x * kTile, o_tmem = tmem + 2 * kTile + x * D;
+      // a step is half a tile: 64 rows of 128 bytes per panel
+      auto issue_s = [&](int half, int slot) {
+        const uint64_t b = desc_advance(k_desc, slot * Sm::kTileBytes + half * (kStep * 128));
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
           const uint32_t off = (i >> 2) * (kTile * 128) + (i & 3) * 32;
-          mma_ss_w(lead, tmem + x * kTile, desc_advance(q_desc, off), desc_advance(b, off), idesc_s, i > 0);
+          mma_ss_w(lead, s_tmem + half * kStep, desc_advance(q_desc, off), desc_advance(b, off), idesc_s, i > 0);
         }
-        mma_commit_w(lead, &sm.s_full[x]);
       };
       auto issue_pv = [&](int half, int slot, bool add) {
-        const uint64_t b = desc_advance(v_desc, slot * Sm::kTileBytes + half * (kTile / 2 * 128));
+        const uint64_t b = desc_advance(v_desc, slot * Sm::kTileBytes + half * (kStep * 128));
 #pragma unroll
-        for (int i = 0; i < kTile / 32; ++i)
-          mma_ts_w(lead, tmem + 2 * kTile + x * D, tmem + x * kTile + half * (kTile / 4) + 8 * i, desc_advance(b, i * 2048), idesc_o, add || i > 0);
+        for (int i = 0; i < kStep / 16; ++i) mma_ts_w(lead, o_tmem, s_tmem + half * kStep + 8 * i, desc_advance(b, i * 2048), idesc_o, add || i > 0);
       };
       // Position in the ring of K(j) is 2j, of V(j) 2j + 1.  Both warps release every slot, whether its keys concern their M-tile or not,
       // and always by a commit.
@@ -470,33 +463,36 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         ok = all_wait(&sm.full[0], 0, abort);
         if (ok) {
           tc_fence_after_sync();
-          if (n > 0) issue_s(0);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            if (half < n) issue_s(half, 0);
+            mma_commit_w(lead, &sm.s_full[x][half]);
+          }
           mma_commit_w(lead, &sm.empty[0]);
           next();
         }
       }
 #pragma unroll 1
       for (int j = 0; ok && j < n_tiles; ++j) {
-        // V(j), and K(j + 1) ahead of the second half of P(j), whose arrival the softmax threads' next S hangs on
         const int v_slot = slot;
         const bool more = j + 1 < n_tiles;
         ok = all_wait(&sm.full[v_slot], phase, abort);
         next();
         const int k_slot = slot;
-        if (ok && j < n) {
-          ok = all_wait(&sm.p_full[x][0], j & 1, abort);
+        if (ok && more) ok = all_wait(&sm.full[k_slot], phase, abort);
+#pragma unroll 1
+        for (int half = 0; ok && half < 2; ++half) {
+          const int step = 2 * j + half;
+          if (step >= n) break;
+          ok = all_wait(&sm.p_full[x][half], j & 1, abort);
           if (!ok) break;
           tc_fence_after_sync();
-          issue_pv(0, v_slot, j > 0);
+          issue_pv(half, v_slot, step > 0);
+          if (step + 2 < n) issue_s(half, k_slot);
+          mma_commit_w(lead, &sm.s_full[x][half]);
         }
-        if (ok && more) ok = all_wait(&sm.full[k_slot], phase, abort);
-        if (ok && j < n) ok = all_wait(&sm.p_full[x][1], j & 1, abort);
         if (!ok) break;
-        tc_fence_after_sync();
-        if (j < n) issue_pv(1, v_slot, true);
-        if (j + 1 < n) issue_s(k_slot);
         mma_commit_w(lead, &sm.empty[v_slot]);
-        if (j + 1 == n) mma_commit_w(lead, &sm.o_full[x]);
         if (more) {
           mma_commit_w(lead, &sm.empty[k_slot]);
           next();
