@@ -80,16 +80,15 @@ __device__ __forceinline__ void e2m1x4_to_bf16(uint32_t w, uint32_t& r0, uint32_
   r1 = __byte_perm(lo, hi, 0x7362) | ((w << 4) & 0x8000u) | ((w << 16) & 0x80000000u);
 }
 
-// Two e4m3 numbers (the low 16 bits) / two e2m1 numbers (the low 8 bits) as an fp16 pair, the lower one first
-__device__ __forceinline__ uint32_t e4m3x2_to_f16(uint32_t x) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(r) : "r"(x));
-  return r;
+// Four e4m3 / eight e2m1 numbers of a word as fp16 pairs, the lowest first
+__device__ __forceinline__ void e4m3x4_to_f16(uint32_t x, uint32_t& r0, uint32_t& r1) {
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
+      : "=r"(r0), "=r"(r1) : "r"(x));
 }
-__device__ __forceinline__ uint32_t e2m1x2_to_f16(uint32_t x) {
-  uint32_t r;
-  asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(r) : "r"(x));
-  return r;
+__device__ __forceinline__ void e2m1x8_to_f16(uint32_t x, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+      : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(x));
 }
 
 constexpr int kCacheBf16 = HGA_CACHE_BF16, kCacheMx8 = HGA_CACHE_MXFP8, kCacheMx4 = HGA_CACHE_MXFP4;

@@ -629,10 +629,12 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
             wide = wide || !(in || sc == 0 || sc == 255);
             const uint32_t mul = pair(in ? e << 10 : sc == 255 ? 0x7e00u : 0u);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < 4; ++k) {
+              if (FMT == kCacheMx8) e4m3x4_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1]);
+              else e2m1x8_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1], o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
 #pragma unroll
-              for (int y = 0; y < kPairs; ++y)
-                o[k * kPairs + y] = mul_f16x2(FMT == kCacheMx8 ? e4m3x2_to_f16(q[k] >> (16 * y)) : e2m1x2_to_f16(q[k] >> (8 * y)), mul);
+              for (int y = 0; y < kPairs; ++y) o[k * kPairs + y] = mul_f16x2(o[k * kPairs + y], mul);
+            }
           } else {
             const uint32_t mul = pair(scale_bits(sc));
 #pragma unroll

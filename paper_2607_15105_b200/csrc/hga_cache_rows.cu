@@ -5,11 +5,11 @@
 // cp.async fills ahead, and work on them with warp-level matrix instructions: nothing is shared between warps until the end, where
 // their sums meet.  What bounds it is the keys' and values' bytes; tcgen05's 128-row tiles would be padding here.
 //
-// How the operands come about: S = Q K^T; O^T = V^T P^T, because then P's registers are those of S as they are.  bf16: the registers
-// of K and (transposed) of V are what ldmatrix delivers.  Quantised: the order in which a product sums over its inner axis
-// is free, and so is the order of the rows of its result, so a lane (g, c) = (lane / 4, lane % 4) takes eight numbers of every
-// block of key g, and Q's registers are laid out for the same order; of V it takes the columns g D/8 .. of the keys 2c, 2c+1,
-// 2c+8, 2c+9 and pairs these up.
+// How the operands come about: S^T = K Q^T and O^T = V^T P^T, so that the few query rows are the short side (8 or 16) of both products;
+// between them P^T is transposed in registers.  bf16: the registers of K and (transposed) of V are what ldmatrix delivers.
+// Quantised: the order in which a product sums over its inner axis is free, and so is the order of the rows of its result, so a lane
+// (g, c) = (lane / 4, lane % 4) takes eight numbers of every block of the keys g and g + 8, and Q's registers are laid out for the same
+// order; of V it takes the columns g D/8 .. of the keys 2c, 2c+1, 2c+8, 2c+9 and pairs these up.
 //
 // Quantised pages are multiplied as fp16, into which the converter instructions go, and which holds e4m3 and e2m1 exactly.  K without
 // its scales: they multiply the sums over a block (fp32) afterwards; Q is brought to fp16 by a power of two per row, exactly but for
@@ -78,6 +78,11 @@ __device__ __forceinline__ uint32_t f16_to_bf16(uint32_t x) {
   return pack_bf16(f.x, f.y);
 }
 
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {      // of a matrix of pairs, a row in four lanes
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -213,15 +218,19 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
 
   // Q in registers, in K's order; a row's last visible key; what its logits are multiplied by
   uint32_t qa[D / 16][2 * NT];
-  int lim[NT];
-  float to_log2[NT];
+  int lim[NT][2];                       // of rows 2c, 2c + 1
+  float to_log2[NT][2];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = row0 + n * 8 + 2 * c + i;
+      lim[n][i] = row < rows ? min(pos0 + dm.by_G(row), s.keys - 1) : 0x7fffffff;
+    }
+    float per_row = dm.scale * 1.44269504088896340736f;      // of row g
     const int row = row0 + n * 8 + g;
     const bool real = row < rows;
     const int t = real ? dm.by_G(row) : 0, head = h * dm.G + (row - t * dm.G);
-    lim[n] = real ? min(pos0 + t, s.keys - 1) : 0x7fffffff;
-    to_log2[n] = dm.scale * 1.44269504088896340736f;
     const uint16_t* q = Q + (s.q0 + t) * dm.qs[0] + head * dm.qs[1];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
@@ -247,13 +256,15 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
       // the row's largest to 2^14 .. 2^15, by a power of two that fp32 holds (and its inverse)
       const int up = max(min(127 + 14 - (int)(big >> 7), 100), -100);
       const float f = __uint_as_float((uint32_t)(127 + up) << 23);
-      to_log2[n] *= __uint_as_float((uint32_t)(127 - up) << 23);
+      per_row *= __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
 #pragma unroll
         for (int k = 2 * n; k < 2 * n + 2; ++k)
           qa[i][k] = pack_f16(__uint_as_float(qa[i][k] << 16) * f, __uint_as_float(qa[i][k] & 0xffff0000u) * f);
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) to_log2[n][i] = __shfl_sync(0xffffffffu, per_row, 8 * c + 4 * i);
   }
   all_there = __syncthreads_and(all_there);
 
@@ -291,11 +302,11 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
     }
   };
 
-  float o[NT][D / 16][4], ones[NT][4], m[NT], l[NT];
+  float o[NT][D / 16][4], ones[NT][4], m[NT][2], l[NT][2];      // columns 2c, 2c + 1
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    m[n] = kNoRef;
-    l[n] = 0.f;
+    m[n][0] = m[n][1] = kNoRef;
+    l[n][0] = l[n][1] = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) ones[n][i] = 0.f;
 #pragma unroll
@@ -379,44 +390,53 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
       __syncwarp();
     }
 
-    float x[2 * SUB][4];
+    // keys (b 16 + g) and (.. + 8), rows 2c and 2c + 1
+    float x[SUB][NT][4];
 #pragma unroll
-    for (int u = 0; u < 2 * SUB; ++u) {
+    for (int b = 0; b < SUB; ++b) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[u][i] = 0.f;
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[b][n][i] = 0.f;
       if (!kScaled) {
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {        // 32 elements: four 8 x 8 matrices of keys u * 8 ..
-          uint32_t b[4];
-          ldmatrix4<false>(b, buf_addr + (u * 8 + (lane & 7)) * Rg::kRow + Rg::k_piece(lane & 7, 4 * i + (lane >> 3)) * 16);
-          mma_bf16(x[u], qa[2 * i][0], NT == 2 ? qa[2 * i][2 % (2 * NT)] : 0u, qa[2 * i][1], NT == 2 ? qa[2 * i][3 % (2 * NT)] : 0u, b[0], b[1]);
-          mma_bf16(x[u], qa[2 * i + 1][0], NT == 2 ? qa[2 * i + 1][2 % (2 * NT)] : 0u, qa[2 * i + 1][1],
-                   NT == 2 ? qa[2 * i + 1][3 % (2 * NT)] : 0u, b[2], b[3]);
+        for (int i = 0; i < D / 16; ++i) {        // (keys 0-7, 16i ..), (keys 8-15, 16i ..), (keys 0-7, 16i + 8 ..), (keys 8-15, 16i + 8 ..)
+          uint32_t k[4];
+          const int r = b * 16 + (lane & 15);
+          ldmatrix4<false>(k, buf_addr + r * Rg::kRow + Rg::k_piece(r, 2 * i + (lane >> 4)) * 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_bf16(x[b][n], k[0], k[1], k[2], k[3], qa[i][2 * n], qa[i][2 * n + 1]);
         }
       } else {
-        float f0[NB], f1[NB];                     // of keys 2c, 2c + 1
-        lds<NB>(reinterpret_cast<uint32_t*>(f0), reinterpret_cast<const uint8_t*>(k_factor + (u * 8 + 2 * c) * NB));
-        lds<NB>(reinterpret_cast<uint32_t*>(f1), reinterpret_cast<const uint8_t*>(k_factor + (u * 8 + 2 * c + 1) * NB));
-        const int r = u * 8 + g;
+        float f[2][NB];                           // of keys g, g + 8
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          float acc[4];
-          uint32_t k[4];
-          if (FMT == kCacheMx8) {
-            uint32_t w[2];
-            lds<2>(w, buf + r * Rg::kRow + Rg::k_piece(r, 2 * b + (c >> 1)) * 16 + (c & 1) * 8);
-            k[0] = e4m3x2_to_f16(w[0]); k[1] = e4m3x2_to_f16(w[0] >> 16);
-            k[2] = e4m3x2_to_f16(w[1]); k[3] = e4m3x2_to_f16(w[1] >> 16);
-          } else {
-            uint32_t w;
-            lds<1>(&w, buf + r * Rg::kRow + Rg::k_piece(r, b) * 16 + c * 4);
-            k[0] = e2m1x2_to_f16(w); k[1] = e2m1x2_to_f16(w >> 8); k[2] = e2m1x2_to_f16(w >> 16); k[3] = e2m1x2_to_f16(w >> 24);
+        for (int i = 0; i < 2; ++i)
+          lds<NB>(reinterpret_cast<uint32_t*>(f[i]), reinterpret_cast<const uint8_t*>(k_factor + (b * 16 + 8 * i + g) * NB));
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+          uint32_t k[2][4];                       // [16 elements][..]
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int r = b * 16 + 8 * i + g;
+            if (FMT == kCacheMx8) {
+              uint32_t w[2];
+              lds<2>(w, buf + r * Rg::kRow + Rg::k_piece(r, 2 * t + (c >> 1)) * 16 + (c & 1) * 8);
+              e4m3x4_to_f16(w[0], k[0][i], k[0][2 + i]);
+              e4m3x4_to_f16(w[1], k[1][i], k[1][2 + i]);
+            } else {
+              uint32_t w;
+              lds<1>(&w, buf + r * Rg::kRow + Rg::k_piece(r, t) * 16 + c * 4);
+              e2m1x8_to_f16(w, k[0][i], k[0][2 + i], k[1][i], k[1][2 + i]);
+            }
           }
-          mma_f16_zero(acc, qa[2 * b][0], NT == 2 ? qa[2 * b][2 % (2 * NT)] : 0u, qa[2 * b][1], NT == 2 ? qa[2 * b][3 % (2 * NT)] : 0u, k[0], k[1]);
-          mma_f16(acc, qa[2 * b + 1][0], NT == 2 ? qa[2 * b + 1][2 % (2 * NT)] : 0u, qa[2 * b + 1][1],
-                  NT == 2 ? qa[2 * b + 1][3 % (2 * NT)] : 0u, k[2], k[3]);
 #pragma unroll
-          for (int i = 0; i < 2 * NT; ++i) x[u][i] = fmaf(acc[i], (i & 1) ? f1[b] : f0[b], x[u][i]);
+          for (int n = 0; n < NT; ++n) {
+            float acc[4];
+            mma_f16_zero(acc, k[0][0], k[0][1], k[0][2], k[0][3], qa[2 * t][2 * n], qa[2 * t][2 * n + 1]);
+            mma_f16(acc, k[1][0], k[1][1], k[1][2], k[1][3], qa[2 * t + 1][2 * n], qa[2 * t + 1][2 * n + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[b][n][i] = fmaf(acc[i], f[i >> 1][t], x[b][n][i]);
+          }
         }
       }
     }
@@ -424,55 +444,65 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
     // hidden logits -inf
     if (masked) {
 #pragma unroll
-      for (int u = 0; u < 2 * SUB; ++u)
+      for (int b = 0; b < SUB; ++b)
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i)
-          if (base + u * 8 + 2 * c + (i & 1) > lim[i >> 1] || base + u * 8 + 2 * c + (i & 1) >= k1) x[u][i] = -INFINITY;
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = base + b * 16 + 8 * (i >> 1) + g;
+            if (key > lim[n][i & 1] || key >= k1) x[b][n][i] = -INFINITY;
+          }
     }
-    float top[NT];
+    float top[NT][2];
     bool raise = false;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      top[n] = x[0][2 * n];
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int u = 0; u < 2 * SUB; ++u) top[n] = fmaxf(top[n], fmaxf(x[u][2 * n], x[u][2 * n + 1]));
-      top[n] *= to_log2[n];             // (in units of log2)
-      raise = raise || top[n] > m[n] + kSlack;
-    }
+      for (int i = 0; i < 2; ++i) {
+        top[n][i] = fmaxf(x[0][n][i], x[0][n][i + 2]);
+#pragma unroll
+        for (int b = 1; b < SUB; ++b) top[n][i] = fmaxf(top[n][i], fmaxf(x[b][n][i], x[b][n][i + 2]));
+        top[n][i] *= to_log2[n][i];     // (in units of log2)
+        raise = raise || top[n][i] > m[n][i] + kSlack;
+      }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float now = top[n];
-        now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 1));
-        now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 2));
-        now = fmaxf(m[n], now - kLow);
-        const float f = fast_exp2(m[n] - now);
-        m[n] = now;
-        l[n] *= f;
-        const float f0 = __shfl_sync(0xffffffffu, f, 8 * c), f1 = __shfl_sync(0xffffffffu, f, 8 * c + 4);      // of rows 2c, 2c + 1
+        float f[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ones[n][i] *= (i & 1) ? f1 : f0;
+        for (int i = 0; i < 2; ++i) {
+          float now = top[n][i];
+#pragma unroll
+          for (int k = 4; k < 32; k <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, k));
+          now = fmaxf(m[n][i], now - kLow);
+          f[i] = fast_exp2(m[n][i] - now);
+          m[n][i] = now;
+          l[n][i] *= f[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ones[n][i] *= f[i & 1];
 #pragma unroll
         for (int t = 0; t < D / 16; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[n][t][i] *= (i & 1) ? f1 : f0;
+          for (int i = 0; i < 4; ++i) o[n][t][i] *= f[i & 1];
       }
     }
 #pragma unroll
-    for (int u = 0; u < 2 * SUB; ++u)
+    for (int b = 0; b < SUB; ++b)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        x[u][2 * n] = fast_exp2(fmaf(x[u][2 * n], to_log2[n], -m[n]));
-        x[u][2 * n + 1] = fast_exp2(fmaf(x[u][2 * n + 1], to_log2[n], -m[n]));
-        l[n] += x[u][2 * n] + x[u][2 * n + 1];
-      }
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[b][n][i] = fast_exp2(fmaf(x[b][n][i], to_log2[n][i & 1], -m[n][i & 1]));
+          l[n][i & 1] += x[b][n][i];
+        }
 
     if (!kScaled) {
       uint32_t p[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) p[n][u] = pack_bf16(x[u][2 * n], x[u][2 * n + 1]);
+        for (int u = 0; u < 2; ++u) p[n][u] = transpose8x8(pack_bf16(x[0][n][2 * u], x[0][n][2 * u + 1]));
 #pragma unroll
       for (int n = 0; n < NT; ++n) mma_bf16(ones[n], 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u, p[n][0], p[n][1]);
 #pragma unroll
@@ -516,7 +546,7 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
           for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-              p[n][u] = kF16 ? pack_f16(x[2 * b + u][2 * n], x[2 * b + u][2 * n + 1]) : pack_bf16(x[2 * b + u][2 * n], x[2 * b + u][2 * n + 1]);
+              p[n][u] = transpose8x8(kF16 ? pack_f16(x[b][n][2 * u], x[b][n][2 * u + 1]) : pack_bf16(x[b][n][2 * u], x[b][n][2 * u + 1]));
             constexpr uint32_t one = kF16 ? 0x3c003c00u : 0x3f803f80u;
             mma<kF16>(ones[n], one, one, one, one, p[n][0], p[n][1]);
             if (!kF16)
@@ -530,13 +560,14 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
               const uint32_t u0 = w[2 * half][t2 / (FMT == kCacheMx8 ? 1 : 2)], u1 = w[2 * half + 1][t2 / (FMT == kCacheMx8 ? 1 : 2)];
               uint32_t y[4];
               if (FMT == kCacheMx8) {
-                const uint32_t lo = __byte_perm(u0, u1, 0x5140), hi = __byte_perm(u0, u1, 0x7362);
-                y[0] = e4m3x2_to_f16(lo); y[1] = e4m3x2_to_f16(lo >> 16); y[2] = e4m3x2_to_f16(hi); y[3] = e4m3x2_to_f16(hi >> 16);
+                e4m3x4_to_f16(__byte_perm(u0, u1, 0x5140), y[0], y[1]);
+                e4m3x4_to_f16(__byte_perm(u0, u1, 0x7362), y[2], y[3]);
               } else {
                 const uint32_t even = (u0 & 0x0f0f0f0fu) | ((u1 << 4) & 0xf0f0f0f0u), odd = ((u0 >> 4) & 0x0f0f0f0fu) | (u1 & 0xf0f0f0f0u);
-                const int sh = (t2 & 1) * 16;
-                y[0] = e2m1x2_to_f16(even >> sh); y[1] = e2m1x2_to_f16(odd >> sh);
-                y[2] = e2m1x2_to_f16(even >> (sh + 8)); y[3] = e2m1x2_to_f16(odd >> (sh + 8));
+                uint32_t e[4], d[4];               // (of a word each; the other half serves the next t2)
+                e2m1x8_to_f16(even, e[0], e[1], e[2], e[3]);
+                e2m1x8_to_f16(odd, d[0], d[1], d[2], d[3]);
+                y[0] = e[2 * (t2 & 1)]; y[1] = d[2 * (t2 & 1)]; y[2] = e[2 * (t2 & 1) + 1]; y[3] = d[2 * (t2 & 1) + 1];
               }
 #pragma unroll
               for (int k = 0; k < 4; ++k) a[k >> 1][2 * half + (k & 1)] = kF16 ? mul_f16x2(y[k], mul[half]) : mul_bf16x2(f16_to_bf16(y[k]), mul[half]);
@@ -558,10 +589,16 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
   // the warps' sums meet (each warp's in the place of its ring)
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
-    l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
-    if (c == 0) { sm_m[warp][n * 8 + g] = m[n]; sm_l[warp][n * 8 + g] = l[n]; }
-    if (g == 0) { sm_r[warp][n * 8 + 2 * c] = ones[n][0]; sm_r[warp][n * 8 + 2 * c + 1] = ones[n][1]; }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int k = 4; k < 32; k <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], k);
+      if (g == 0) {
+        sm_m[warp][n * 8 + 2 * c + i] = m[n][i];
+        sm_l[warp][n * 8 + 2 * c + i] = l[n][i];
+        sm_r[warp][n * 8 + 2 * c + i] = ones[n][i];
+      }
+    }
     float* dst = reinterpret_cast<float*>(ring) + (n * 8 + 2 * c) * kPitch;
     constexpr float down = 1.f / (float)(1 << kLift);
 #pragma unroll
@@ -619,18 +656,20 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
   }
 }
 
-// Joins the parts of every row: one warp per (token, query head)
+// Joins the parts of every row: a CTA per (token, query head), whose warps share the parts out among them
+constexpr int kJoinWarps = 8;
+
 template <int D>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kJoinWarps * 32)
 k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens,
              const float* __restrict__ part_o, uint16_t* __restrict__ O, float* __restrict__ LSE) {
-  const int64_t all_rows = (int64_t)dm.n_tokens * dm.Hq;
-  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
+  constexpr int N = D / 32;
+  __shared__ float sm_o[kJoinWarps][D], sm_l[kJoinWarps], sm_r[kJoinWarps], sm_m[kJoinWarps];
+  const int64_t all_rows = (int64_t)dm.n_tokens * dm.Hq, row = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tok = blockIdx.x / dm.Hq, head = blockIdx.x - tok * dm.Hq;
   pdl_wait();
   pdl_launch_dependents();
-  if (row >= all_rows) return;
-  const int tok = (int)(row / dm.Hq), head = (int)(row - (int64_t)tok * dm.Hq);
   int lo = 0, hi = dm.n_seq;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -641,16 +680,16 @@ k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict_
   const int last = min(s.len - s.n_all + (tok - s.q0), s.keys - 1);
   const int parts = last < 0 ? 0 : last / sp.keys + 1;
   const float4* ml = reinterpret_cast<const float4*>(part_o + sp.parts * all_rows * D);
+  // each warp against the largest reference of its own parts
   float top = kNoRef;
-  for (int i = lane; i < parts; i += 32) top = fmaxf(top, ml[i * all_rows + row].x);
+  for (int i = warp + kJoinWarps * lane; i < parts; i += kJoinWarps * 32) top = fmaxf(top, ml[i * all_rows + row].x);
 #pragma unroll
   for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
-  constexpr int N = D / 32;
   float sum[N], ls = 0.f, lr = 0.f;
 #pragma unroll
   for (int e = 0; e < N; ++e) sum[e] = 0.f;
 #pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
+  for (int i = warp; i < parts; i += kJoinWarps) {
     const float4 x = ml[i * all_rows + row];
     const float f = fast_exp2(x.x - top);
     ls += f * x.y;
@@ -663,11 +702,27 @@ k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict_
       sum[e + 1] += f * y.y;
     }
   }
-  const float inv = lr > 0.f ? 1.f / lr : (lr == 0.f ? 0.f : lr);
-  uint32_t* dst = reinterpret_cast<uint32_t*>(O + tok * dm.os[0] + head * dm.os[1] + lane * N);
 #pragma unroll
-  for (int e = 0; e < N; e += 2) dst[e / 2] = pack_bf16(sum[e] * inv, sum[e + 1] * inv);
-  if (LSE && lane == 0) LSE[row] = ls > 0.f ? (top + log2f(ls)) * 0.69314718055994530942f : (ls == 0.f ? -INFINITY : ls);
+  for (int e = 0; e < N; ++e) sm_o[warp][lane * N + e] = sum[e];
+  if (lane == 0) { sm_m[warp] = top; sm_l[warp] = ls; sm_r[warp] = lr; }
+  __syncthreads();
+  if (threadIdx.x >= D / 2) return;
+  top = sm_m[0];
+#pragma unroll
+  for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, sm_m[w]);
+  float a = 0.f, b = 0.f;
+  ls = lr = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float f = fast_exp2(sm_m[w] - top);
+    a += f * sm_o[w][2 * threadIdx.x];
+    b += f * sm_o[w][2 * threadIdx.x + 1];
+    ls += f * sm_l[w];
+    lr += f * sm_r[w];
+  }
+  const float inv = lr > 0.f ? 1.f / lr : (lr == 0.f ? 0.f : lr);
+  *reinterpret_cast<uint32_t*>(O + tok * dm.os[0] + head * dm.os[1] + 2 * threadIdx.x) = pack_bf16(a * inv, b * inv);
+  if (LSE && threadIdx.x == 0) LSE[row] = ls > 0.f ? (top + log2f(ls)) * 0.69314718055994530942f : (ls == 0.f ? -INFINITY : ls);
 }
 
 template <int FMT, int D, int NT>
@@ -695,7 +750,7 @@ int rows_of(const CacheDims& dm, const CacheSplit& sp, const void* Q, const int3
 // not show.  (Sequences are usually shorter; CTAs without keys cost next to nothing.)
 CacheSplit cache_rows_split(const CacheDims& dm) {
   const int64_t tiles = (int64_t)dm.n_seq * dm.Hkv * ((dm.max_new * dm.G + 15) / 16);
-  const int64_t want = (dm.max_keys * tiles + 148 * 6 - 1) / (148 * 6);
+  const int64_t want = (dm.max_keys * tiles + 148 * 3 - 1) / (148 * 3);
   CacheSplit sp;
   sp.keys = (int)std::min<int64_t>(std::max<int64_t>((want + 127) / 128 * 128, 256), 2048);
   sp.parts = std::max((dm.max_keys + sp.keys - 1) / sp.keys, 1);
@@ -705,7 +760,7 @@ CacheSplit cache_rows_split(const CacheDims& dm) {
 int launch_cache_join(const CacheDims& dm, const CacheSplit& sp, const int32_t* cu_q, const int32_t* seq_lens, const void* workspace,
                       void* O, float* LSE, cudaStream_t st) {
   const int64_t rows = (int64_t)dm.n_tokens * dm.Hq;
-  PdlLaunch cfg(dim3((unsigned)((rows + 7) / 8)), 256, 0, st, 0);
+  PdlLaunch cfg(dim3((unsigned)rows), kJoinWarps * 32, 0, st, 0);
   const cudaError_t e = cudaLaunchKernelEx(&cfg.c, dm.d == 128 ? k_cache_join<128> : k_cache_join<64>, dm, sp, cu_q, seq_lens,
                                            (const float*)workspace, (uint16_t*)O, LSE);
   count_launch(HGA_KERNELS_CACHE_ROWS);
