@@ -10,7 +10,7 @@
 //   warps 0-3, 4-7   softmax and epilogue of M-tile 0 and 1
 //   warps 8, 9       issue the GEMMs of M-tile 0 and 1
 //   warps 10, 11     copy K and V tiles by TMA, a box per page part (quantised pages: as they are, warp 10 alone)
-//   warps 12-15      quantised pages: convert K and V tiles; bf16 pages: clean the last V tiles
+//   warps 12-15      bf16 pages: clean the last V tiles; quantised: convert K and V tiles
 //
 // Quantised pages are multiplied as fp16, into which the converter instructions go and which holds e4m3 and e2m1 with their scales
 // exactly while these lie in a range of 2^22 (e4m3; Q is brought to fp16 by a power of two per row, exactly but for numbers 2^-29 of
@@ -32,6 +32,10 @@ using namespace sm100;
 namespace {
 
 constexpr int kThreads = 512;
+// Registers of a thread of the softmax warps, of GEMMs and copies, of the rest; the launch has 128 for each.
+constexpr int kSoftmaxRegs = 184, kIssueRegs = 48, kRestRegs = 96;
+static_assert(2 * kSoftmaxRegs + kIssueRegs + kRestRegs <= 4 * 128, "registers of the block");
+constexpr int kFill = 4;                   // warps that convert or clean
 constexpr int kTile = 128;                 // rows of an M-tile, keys of a tile
 constexpr int kStep = 64;                  // keys of a step
 constexpr uint32_t kTmemCols = 512;
@@ -49,7 +53,7 @@ struct Smem {
   uint8_t q[2][kTileBytes];                // [panel of 64 elements][row][128 bytes], 128-byte swizzle, as all tiles
   uint8_t ring[kSlots][kTileBytes];        // K and V tiles in turn
   uint8_t raw[2][kScaled ? kRaw + kRawScales : 128];      // quantised tiles as they lie in their pages, rows one behind the other, and their scales
-  uint64_t full[kSlots], empty[kSlots];    // full: four arrivals, whoever fills the slot
+  uint64_t full[kSlots], empty[kSlots];    // full: one arrival of each of the filling warps (four for the copying ones)
   uint64_t raw_full[kSlots];               // what has to be converted has arrived (two); a V tile that has to be cleaned (any slot)
   uint64_t raw_empty[2];
   // s_full, p_full: of M-tile x's buffer b.  s_full for the t-th time: S of step 2 t + b is there, if there is such a step, and P V of
@@ -156,12 +160,12 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   }
   auto init_barriers = [&]() {
     for (int i = 0; i < NS; ++i) {
-      mbar_init(&sm.full[i], 4);
+      mbar_init(&sm.full[i], kFill);
       mbar_init(&sm.empty[i], 2);
       mbar_init(&sm.raw_full[i], 1);
     }
     for (int x = 0; x < 2; ++x) {
-      mbar_init(&sm.raw_empty[x], 4);
+      mbar_init(&sm.raw_empty[x], kFill);
       for (int b = 0; b < 2; ++b) {
         mbar_init(&sm.s_full[x][b], 1);
         mbar_init(&sm.p_full[x][b], 4);
@@ -271,7 +275,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int x = warp >> 2, r = tid & 127;
     const int t = dm.by_G(r), tok = x * plan.tokens + t;
     const bool real = t < plan.tokens && tok < n_tok;
@@ -427,7 +431,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         *reinterpret_cast<float4*>(part_o + plan.sp.parts * all_rows * D + (part * all_rows + out_row) * 4) = make_float4(m, l, l, 0.f);
     }
   } else if (warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
     do {
     if (warp < 10) {
       // ---------------------------------------------------------------- GEMMs (the whole warp stays together, one lane issues)
@@ -559,7 +563,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
     } while (again());
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
     const int w = warp - 12;
     do {
     bool strange = false;
@@ -597,67 +601,75 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
     } else {
       // ---------------------------------------------------------------- quantised tiles: converted from one buffer into another
-      constexpr int LPR = cache_row_bytes(FMT, D) / 16;        // lanes of a row, and 16-byte pieces that a thread has of a tile
-      constexpr int RPI = 32 / LPR;                            // rows of a warp's access
-      const int in_row = lane % LPR;
+      constexpr int LPR = cache_row_bytes(FMT, D) / 16;        // lanes of a row
+      constexpr int RPI = 32 / LPR, kRows = kFill * RPI;       // rows of a warp's access, of all warps' (a multiple of 8)
+      constexpr int kPairs = FMT == kCacheMx8 ? 2 : 4;         // 16-byte pieces of bf16 or fp16 that a lane's 16 bytes become
+      const int in_row = lane % LPR, r0 = w * RPI + lane / LPR;
       bool wide = false;
+      auto convert = [&](auto as_f16) {
+        constexpr bool kF16 = decltype(as_f16)::value;
 #pragma unroll 1
-      for (int i_ring = 0; i_ring < 2 * n_tiles; ++i_ring) {
-        const int use = i_ring / NS, slot = i_ring - use * NS, j = i_ring >> 1;
-        const bool is_v = i_ring & 1;
-        if (!all_wait(&sm.raw_full[i_ring & 1], (i_ring >> 1) & 1, abort) || !all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
-        const uint8_t* src = sm.raw[i_ring & 1];
-        const int end = k1 - (k0 + j * kTile), hidden = is_v ? first_lim - (k0 + j * kTile) : kTile;      // rows from `end` on are none
-#pragma unroll 4
-        for (int i = 0; i < LPR; ++i) {
-          const int r = i * (4 * RPI) + w * RPI + lane / LPR;
-          uint4 y = *reinterpret_cast<const uint4*>(src + r * cache_row_bytes(FMT, D) + in_row * 16);
-          uint32_t sc = src[Sm::kRaw + r * (D / 32) + (FMT == kCacheMx8 ? in_row >> 1 : in_row)];
-          if (r >= end) {
-            y = make_uint4(0, 0, 0, 0);
-            sc = 0;
-          }
-          if (sc == 255 && r > hidden) { sc = 0; strange = true; }
-          const uint32_t q[4] = {y.x, y.y, y.z, y.w};
-          // pairs of neighbours: four of a word of e2m1, two of e4m3
-          constexpr int kPairs = FMT == kCacheMx8 ? 2 : 4;
-          uint32_t o[4 * kPairs];
-          if (f16) {
-            // (2^-127 counts as zero: so do numbers below 2^-118)
-            const uint32_t e = sc - (127 - kLift - 15);
-            const bool in = e - 1 < kTop + 15;
-            wide = wide || !(in || sc == 0 || sc == 255);
-            const uint32_t mul = pair(in ? e << 10 : sc == 255 ? 0x7e00u : 0u);
+        for (int i_ring = 0; i_ring < 2 * n_tiles; ++i_ring) {
+          const int use = i_ring / NS, slot = i_ring - use * NS, j = i_ring >> 1;
+          const bool is_v = i_ring & 1;
+          if (!all_wait(&sm.raw_full[i_ring & 1], (i_ring >> 1) & 1, abort) || !all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
+          const uint8_t* src = sm.raw[i_ring & 1] + r0 * cache_row_bytes(FMT, D) + in_row * 16;
+          const uint8_t* scales = sm.raw[i_ring & 1] + Sm::kRaw + r0 * (D / 32) + (FMT == kCacheMx8 ? in_row >> 1 : in_row);
+          uint8_t* dst = sm.ring[slot];
+          const int end = k1 - (k0 + j * kTile) - r0, hidden = is_v ? first_lim - (k0 + j * kTile) - r0 : kTile;      // rows from `end` on are none
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if (FMT == kCacheMx8) e4m3x4_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1]);
-              else e2m1x8_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1], o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
-#pragma unroll
-              for (int y = 0; y < kPairs; ++y) o[k * kPairs + y] = mul_f16x2(o[k * kPairs + y], mul);
+          for (int i = 0; i < kTile / kRows; ++i) {
+            uint4 y = *reinterpret_cast<const uint4*>(src + i * kRows * cache_row_bytes(FMT, D));
+            uint32_t sc = scales[i * kRows * (D / 32)];
+            if (i * kRows >= end) {
+              y = make_uint4(0, 0, 0, 0);
+              sc = 127;
             }
-          } else {
-            const uint32_t mul = pair(scale_bits(sc));
+            const uint32_t q[4] = {y.x, y.y, y.z, y.w};
+            uint32_t o[4 * kPairs], mul;
+            if (kF16) {
+              const uint32_t e = sc - (127 - kLift - 15);
+              mul = e * 0x04000400u;
+              if (e - 1 >= kTop + 15) {          // out of range: zeros (2^-127 counts as zero), NaN, or a number that is too large or small
+                if (sc == 255 && i * kRows > hidden) { sc = 0; strange = true; }
+                mul = sc == 255 ? 0x7e007e00u : 0u;
+                wide = wide || (sc != 0 && sc != 255);
+              }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if (FMT == kCacheMx8) {
-                o[k * kPairs] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x1404)), kTwo120), mul);
-                o[k * kPairs + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x3424)), kTwo120), mul);
-              } else {
-                e2m1x4_to_bf16(q[k] & 0xffffu, o[k * kPairs], o[k * kPairs + 1]);
-                e2m1x4_to_bf16(q[k] >> 16, o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
+              for (int k = 0; k < 4; ++k) {
+                if (FMT == kCacheMx8) e4m3x4_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1]);
+                else e2m1x8_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1], o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
 #pragma unroll
-                for (int y = 0; y < kPairs; ++y) o[k * kPairs + y] = mul_bf16x2(o[k * kPairs + y], mul);
+                for (int z = 0; z < kPairs; ++z) o[k * kPairs + z] = mul_f16x2(o[k * kPairs + z], mul);
+              }
+            } else {
+              if (sc == 255 && i * kRows > hidden) { sc = 0; strange = true; }
+              mul = pair(scale_bits(sc));
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                if (FMT == kCacheMx8) {
+                  o[k * kPairs] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x1404)), kTwo120), mul);
+                  o[k * kPairs + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x3424)), kTwo120), mul);
+                } else {
+                  e2m1x4_to_bf16(q[k] & 0xffffu, o[k * kPairs], o[k * kPairs + 1]);
+                  e2m1x4_to_bf16(q[k] >> 16, o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
+#pragma unroll
+                  for (int z = 0; z < kPairs; ++z) o[k * kPairs + z] = mul_bf16x2(o[k * kPairs + z], mul);
+                }
               }
             }
-          }
+            // (Storing the pieces so that no two lanes meet a bank takes selections that cost more than the conflicts: 581 against 567 us.)
 #pragma unroll
-          for (int k = 0; k < kPairs; ++k)
-            *reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, kPairs * in_row + k)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            for (int k = 0; k < kPairs; ++k)
+              *reinterpret_cast<uint4*>(dst + piece<D>(r0, kPairs * in_row + k) + i * kRows * 128) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          }
+          fence_proxy_async_smem();
+          mbar_arrive_warp(&sm.full[slot]);
+          mbar_arrive_warp(&sm.raw_empty[i_ring & 1]);
         }
-        fence_proxy_async_smem();
-        mbar_arrive_warp(&sm.full[slot]);
-        mbar_arrive_warp(&sm.raw_empty[i_ring & 1]);
-      }
+      };
+      if (f16) convert(std::true_type{});
+      else convert(std::false_type{});
       if (wide) sm.wide = 1;
     }
     if (strange) sm.strange = 1;
