@@ -116,7 +116,7 @@ int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t tok_end
   if ((rc = take_strides(p->out_stride, dm.outs, dense, 8, dm.d))) return rc;
   if (n > 0 && dm.outs[2] == 0) return HGA_ERR_SHAPE;
   if (n == 0) return HGA_OK;
-  if ((n + 31) / 32 * dm.n_seq * dm.Hkv > 0x7fffffff) return HGA_ERR_SHAPE;      // (one CTA has 32 rows or more)
+  if ((n + 31) / 32 * dm.n_seq * dm.Hkv > 0x7fffffff) return HGA_ERR_SHAPE;      // (a CTA has more than 32 rows)
   return launch_cache_read(dm, tok_begin, tok_end, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, K_out, V_out, status_word,
                            (cudaStream_t)stream);
 }

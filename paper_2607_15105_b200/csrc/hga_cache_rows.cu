@@ -746,13 +746,13 @@ int rows_of(const CacheDims& dm, const CacheSplit& sp, const void* Q, const int3
 
 }  // namespace
 
-// Keys per CTA: few enough that the device is full with the sequences as long as max_len says, many enough that a CTA's set-up does
-// not show.  (Sequences are usually shorter; CTAs without keys cost next to nothing.)
+// Keys per CTA: few enough that the device is full once with the sequences as long as max_len says, many enough that a CTA's set-up does
+// not show, and no more than leave three CTAs' shared memory on an SM (e4m3, 32 sequences of 16K: 225 us with 2048, 201 with 1536).  (Sequences are usually shorter; CTAs without keys cost next to nothing.)
 CacheSplit cache_rows_split(const CacheDims& dm) {
   const int64_t tiles = (int64_t)dm.n_seq * dm.Hkv * ((dm.max_new * dm.G + 15) / 16);
   const int64_t want = (dm.max_keys * tiles + 148 * 3 - 1) / (148 * 3);
   CacheSplit sp;
-  sp.keys = (int)std::min<int64_t>(std::max<int64_t>((want + 127) / 128 * 128, 256), 2048);
+  sp.keys = (int)std::min<int64_t>(std::max<int64_t>((want + 127) / 128 * 128, 256), dm.format == kCacheMx8 ? 1536 : 2048);
   sp.parts = std::max((dm.max_keys + sp.keys - 1) / sp.keys, 1);
   return sp;
 }

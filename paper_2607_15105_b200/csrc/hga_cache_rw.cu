@@ -24,11 +24,6 @@ __device__ __forceinline__ int scale_code(uint32_t amax) {
   return max(e - kTopExp + (m > kTopMant ? 1 : 0), 0);
 }
 
-// 2^(127 - s) for s in 0..254 (s = 0: 2^127; larger s may make it subnormal, down to 2^-127)
-__device__ __forceinline__ float inverse_scale(int s) {
-  return s <= 253 ? __uint_as_float((uint32_t)(254 - s) << 23) : __uint_as_float(1u << 22);
-}
-
 // two numbers -> two e4m3 bytes / two e2m1 nibbles (first in the low part), round to nearest even
 __device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
   uint16_t r;
@@ -49,20 +44,26 @@ __device__ __forceinline__ void put8(uint4 x, uint8_t* row, uint8_t* scale, int 
     return;
   }
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t amax = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) amax = max(amax, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-  amax = max(amax, __shfl_xor_sync(mask, amax, 1));
-  amax = max(amax, __shfl_xor_sync(mask, amax, 2));
-  const int s = scale_code<FMT>(amax);
-  // (past 2^127 times this the element would round to 2^128)
-  const float most = FMT == kCacheMx8 ? (s == 247 ? 240.f : 448.f) : (s == 253 ? 3.f : 6.f);
-  const float inv = s == 255 ? 0.f : inverse_scale(s);
+  // magnitudes compare as 16-bit integers do, two at a time
+  uint32_t pairs = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+  pairs = __vmaxu2(pairs, __shfl_xor_sync(mask, pairs, 1));
+  pairs = __vmaxu2(pairs, __shfl_xor_sync(mask, pairs, 2));
+  const int s = scale_code<FMT>(max(pairs & 0xffffu, pairs >> 16));
+  // times 2^(127 - s), in bf16: exact, but for products below 2^-126, which are zeros of the element type anyway
+  const uint32_t inv = pair((uint32_t)(254 - s) << 7);
   float v[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[2 * i] = fminf(fmaxf(bf16_lo(w[i]) * inv, -most), most);
-    v[2 * i + 1] = fminf(fmaxf(bf16_hi(w[i]) * inv, -most), most);
+    const uint32_t y = mul_bf16x2(w[i], inv);
+    v[2 * i] = bf16_lo(y);
+    v[2 * i + 1] = bf16_hi(y);
+  }
+  constexpr int kLast = FMT == kCacheMx8 ? 247 : 253;      // the largest numbers' scale: what would round to 2^128 is rounded toward zero
+  if (s >= kLast) {
+    // (infinities and NaN, s = 255: zeros)
+    constexpr float most = FMT == kCacheMx8 ? 240.f : 3.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = s == 255 ? 0.f : fminf(fmaxf(v[i], -most), most);
   }
   if (FMT == kCacheMx8) {
     *reinterpret_cast<uint2*>(row + c * 8) = make_uint2(to_e4m3x2(v[0], v[1]) | (to_e4m3x2(v[2], v[3]) << 16),
@@ -74,46 +75,66 @@ __device__ __forceinline__ void put8(uint4 x, uint8_t* row, uint8_t* scale, int 
   if ((c & 3) == 0) scale[c >> 2] = (uint8_t)s;
 }
 
+// A CTA takes kWriteRows x 2048 / D consecutive tokens of one head, so that it writes whole sectors of scales, and a thread has all its rows in
+// flight at once.
+constexpr int kWriteRows = 2;
+
 template <int FMT, int D>
 __global__ void __launch_bounds__(256)
 k_cache_write(const CacheDims dm, const uint16_t* __restrict__ K_new, const uint16_t* __restrict__ V_new,
               const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table,
               uint8_t* __restrict__ K, uint8_t* __restrict__ V, uint8_t* __restrict__ K_scale, uint8_t* __restrict__ V_scale,
-              int32_t* status_word, int n_rows) {
-  constexpr int CH = D / 8;                     // threads of a row
-  const int row = (int)(blockIdx.x * (256 / CH) + threadIdx.x / CH), c = threadIdx.x % CH;
+              int32_t* status_word) {
+  constexpr int CH = D / 8, kRows = 256 / CH;   // threads of a row, rows of one access of the CTA
+  const int blk = dm.by_Hkv(blockIdx.x), h = blockIdx.x - blk * dm.Hkv;
+  const int t0 = blk * (kRows * kWriteRows) + threadIdx.x / CH, c = threadIdx.x % CH;
   pdl_wait();
   pdl_launch_dependents();
-  bool here = row < n_rows;                     // (CH divides the warp, so the threads of a row agree)
-  const int t = here ? dm.by_Hkv(row) : 0, h = row - t * dm.Hkv;
-  uint4 k = make_uint4(0, 0, 0, 0), v = k;
-  if (here && K_new) k = *reinterpret_cast<const uint4*>(K_new + t * dm.kns[0] + h * dm.kns[1] + c * 8);
-  if (here && V_new) v = *reinterpret_cast<const uint4*>(V_new + t * dm.vns[0] + h * dm.vns[1] + c * 8);
-  // the sequence of token t: the last one that starts at or ahead of it
+  uint4 k[kWriteRows], v[kWriteRows];
+#pragma unroll
+  for (int u = 0; u < kWriteRows; ++u) {
+    const int64_t t = t0 + u * kRows;
+    k[u] = v[u] = make_uint4(0, 0, 0, 0);
+    if (t < dm.n_tokens && K_new) k[u] = __ldcs(reinterpret_cast<const uint4*>(K_new + t * dm.kns[0] + h * dm.kns[1] + c * 8));
+    if (t < dm.n_tokens && V_new) v[u] = __ldcs(reinterpret_cast<const uint4*>(V_new + t * dm.vns[0] + h * dm.vns[1] + c * 8));
+  }
+  // the sequence of the first token: the last one that starts at or ahead of it
   int lo = 0, hi = dm.n_seq;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (cu_q[mid] <= t) lo = mid; else hi = mid;
+    if (cu_q[mid] <= t0) lo = mid; else hi = mid;
   }
-  const CacheSeq s = cache_seq(dm, cu_q, seq_lens, lo);
-  bool bad = s.bad;
-  here = here && t >= s.q0 && t - s.q0 < s.n;
-  const int pos = s.len - s.n_all + (t - s.q0);
-  here = here && pos >= 0 && pos < dm.max_keys;
-  int page = 0, r = 0;
-  if (here) {
+  bool bad = false;
+  int page[kWriteRows], r[kWriteRows];
+  CacheSeq s = cache_seq(dm, cu_q, seq_lens, lo);
+#pragma unroll
+  for (int u = 0; u < kWriteRows; ++u) {
+    const int t = t0 + u * kRows;
+    page[u] = -1;
+    r[u] = 0;
+    if (t >= dm.n_tokens) continue;
+    while (lo + 1 < dm.n_seq && cu_q[lo + 1] <= t) s = cache_seq(dm, cu_q, seq_lens, ++lo);
+    bad = bad || s.bad;
+    const int pos = s.len - s.n_all + (t - s.q0);
+    if (t < s.q0 || t - s.q0 >= s.n || pos < 0 || pos >= dm.max_keys) continue;
     const int e = dm.by_page(pos);
-    r = pos - e * dm.page;
-    page = table[lo * dm.table_stride + e];
-    if (page < 0 || page >= dm.n_pages) { bad = true; here = false; }
+    r[u] = pos - e * dm.page;
+    page[u] = table[lo * dm.table_stride + e];
+    if (page[u] < 0 || page[u] >= dm.n_pages) { bad = true; page[u] = -1; }
   }
-  if (bad && c == 0 && h == 0) cache_status(status_word, HGA_STATUS_BAD_INDEX);
-  const unsigned mask = __ballot_sync(0xffffffffu, here);
-  if (!here) return;
-  const int64_t srow = (((int64_t)page * dm.Hkv + h) * dm.page + r) * (D / 32);
   constexpr int kUnit = FMT == kCacheBf16 ? 2 : 1;
-  if (K_new) put8<FMT>(k, K + (page * dm.ks[0] + h * dm.ks[1] + r * dm.ks[2]) * kUnit, K_scale + srow, c, mask);
-  if (V_new) put8<FMT>(v, V + (page * dm.vs[0] + h * dm.vs[1] + r * dm.vs[2]) * kUnit, V_scale + srow, c, mask);
+#pragma unroll
+  for (int u = 0; u < kWriteRows; ++u) {
+    const bool here = page[u] >= 0;              // (the threads of a row agree)
+    const unsigned mask = __ballot_sync(0xffffffffu, here);
+    if (here) {
+      const int64_t srow = (((int64_t)page[u] * dm.Hkv + h) * dm.page + r[u]) * (D / 32);
+      if (K_new) put8<FMT>(k[u], K + (page[u] * dm.ks[0] + h * dm.ks[1] + r[u] * dm.ks[2]) * kUnit, K_scale + srow, c, mask);
+      if (V_new) put8<FMT>(v[u], V + (page[u] * dm.vs[0] + h * dm.vs[1] + r[u] * dm.vs[2]) * kUnit, V_scale + srow, c, mask);
+    }
+    __syncwarp();
+  }
+  if (bad && c == 0) cache_status(status_word, HGA_STATUS_BAD_INDEX);
 }
 
 // Eight numbers of a row out of the cache
@@ -122,18 +143,31 @@ template <> struct Raw8<kCacheMx8> { typedef uint2 type; };
 template <> struct Raw8<kCacheMx4> { typedef uint32_t type; };
 
 __device__ __forceinline__ uint4 take8(uint4 x, uint32_t) { return x; }
+// fp16 pairs, each an element's value, as bf16 times 2^(scale - 127).  fp16's sign, exponent and mantissa moved to where bf16 has them are the
+// number times 2^-112.
+__device__ __forceinline__ uint4 scaled(const uint32_t (&x)[4], uint32_t scale) {
+  // (2^(scale - 127 + 112) is beyond bf16 from 143 on; 255 is NaN)
+  const uint32_t first = pair(scale <= 142 ? (scale + 112) << 7 : (127 + 112) << 7);
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = mul_bf16x2((x[i] & 0x80008000u) | ((x[i] >> 3) & 0x0fff0fffu), first);
+  if (scale > 142) {
+    const uint32_t rest = pair(scale_bits(scale));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = mul_bf16x2(y[i], rest);
+  }
+  return make_uint4(y[0], y[1], y[2], y[3]);
+}
 __device__ __forceinline__ uint4 take8(uint2 x, uint32_t scale) {
-  const uint32_t m = pair(scale_bits(scale));
-  auto two = [&](uint32_t w) { return mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(w), kTwo120), m); };
-  return make_uint4(two(__byte_perm(x.x, 0, 0x1404)), two(__byte_perm(x.x, 0, 0x3424)), two(__byte_perm(x.y, 0, 0x1404)),
-                    two(__byte_perm(x.y, 0, 0x3424)));
+  uint32_t y[4];
+  e4m3x4_to_f16(x.x, y[0], y[1]);
+  e4m3x4_to_f16(x.y, y[2], y[3]);
+  return scaled(y, scale);
 }
 __device__ __forceinline__ uint4 take8(uint32_t x, uint32_t scale) {
-  const uint32_t m = pair(scale_bits(scale));
-  uint4 r;
-  e2m1x4_to_bf16(x & 0xffffu, r.x, r.y);
-  e2m1x4_to_bf16(x >> 16, r.z, r.w);
-  return make_uint4(mul_bf16x2(r.x, m), mul_bf16x2(r.y, m), mul_bf16x2(r.z, m), mul_bf16x2(r.w, m));
+  uint32_t y[4];
+  e2m1x8_to_f16(x, y[0], y[1], y[2], y[3]);
+  return scaled(y, scale);
 }
 
 constexpr int kReadRows = 4;      // rows a thread has in flight
@@ -193,11 +227,11 @@ k_cache_read(const CacheDims dm, int tok_begin, int n, const int32_t* __restrict
 template <int FMT, int D>
 int write_of(const CacheDims& dm, const void* K_new, const void* V_new, const int32_t* cu_q, const int32_t* seq_lens,
              const int32_t* table, void* K, void* V, void* K_scale, void* V_scale, int32_t* status_word, cudaStream_t st) {
-  const int n_rows = dm.n_tokens * dm.Hkv, per = 256 / (D / 8);
-  PdlLaunch cfg(dim3((n_rows + per - 1) / per), 256, 0, st, 0);
+  constexpr int per = 256 / (D / 8) * kWriteRows;
+  PdlLaunch cfg(dim3((unsigned)((int64_t)((dm.n_tokens + per - 1) / per) * dm.Hkv)), 256, 0, st, 0);
   const cudaError_t e = cudaLaunchKernelEx(&cfg.c, k_cache_write<FMT, D>, dm, (const uint16_t*)K_new, (const uint16_t*)V_new, cu_q,
                                            seq_lens, table, (uint8_t*)K, (uint8_t*)V, (uint8_t*)K_scale, (uint8_t*)V_scale,
-                                           status_word, n_rows);
+                                           status_word);
   count_launch(HGA_KERNELS_CACHE);
   return record_cuda(e);
 }
