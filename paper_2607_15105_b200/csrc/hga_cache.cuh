@@ -49,6 +49,21 @@ __device__ __forceinline__ CacheSeq cache_seq(const CacheDims& dm, const int32_t
   return cache_seq_of(dm, cu_q[i], cu_q[i + 1], seq_lens[i]);
 }
 
+// The sequence of packed row t: the last one that starts at or ahead of it (0 where none does).  For a whole warp, with the same t:
+// 32 entries of cu_q are looked at at a time.
+__device__ __forceinline__ int find_seq(const int32_t* cu_q, int n_seq, int t) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = n_seq;                    // it is one of lo .. lo + n - 1
+  while (n > 1) {
+    const int step = (n + 31) >> 5, at = lo + lane * step;
+    const unsigned ahead = __ballot_sync(0xffffffffu, lane == 0 || (lane * step < n && cu_q[at] <= t));
+    const int last = 31 - __clz((int)ahead);      // (cu_q does not decrease)
+    n = min(step, n - last * step);
+    lo += last * step;
+  }
+  return lo;
+}
+
 // ----------------------------------------------------------------------------- element formats
 // e4m3 and e2m1 numbers have at most four significant bits and the scales are powers of two, so what is held is a bf16 number and
 // every conversion below is exact.
@@ -101,11 +116,13 @@ int launch_cache_read(const CacheDims& dm, int tok_begin, int tok_end, const int
                       cudaStream_t st);
 
 // How hga_cache_attn shares out a problem: `keys` consecutive keys (a multiple of 128) go to one CTA, `parts` = what the longest
-// sequence has of these; with more than one part the CTAs leave partial results in the workspace, which a second kernel joins.
+// sequence has of these.  Up to eight parts (few rows) form a cluster, whose CTAs join their results through each other's shared memory;
+// otherwise they leave them in the workspace, which a second kernel joins.
 struct CacheSplit {
   int keys, parts;
+  bool cluster;
   size_t bytes(const CacheDims& dm) const {
-    return parts > 1 ? (size_t)parts * dm.n_tokens * dm.Hq * (dm.d + 4) * sizeof(float) : 0;
+    return parts > 1 && !cluster ? (size_t)parts * dm.n_tokens * dm.Hq * (dm.d + 4) * sizeof(float) : 0;
   }
 };
 CacheSplit cache_rows_split(const CacheDims& dm);

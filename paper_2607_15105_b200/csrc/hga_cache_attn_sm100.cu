@@ -708,6 +708,7 @@ Plan plan_of(const CacheDims& dm) {
   const int64_t keys = std::max<int64_t>((dm.max_keys + parts - 1) / parts, 512);
   p.sp.keys = (int)std::min<int64_t>((keys + kTile - 1) / kTile * kTile, 0x7fffff00);
   p.sp.parts = (int)std::max<int64_t>((dm.max_keys + p.sp.keys - 1) / p.sp.keys, 1);
+  p.sp.cluster = false;
   return p;
 }
 

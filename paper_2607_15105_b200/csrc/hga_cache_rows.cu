@@ -114,6 +114,18 @@ __device__ __forceinline__ void lds(uint32_t* w, const uint8_t* p) {
   }
 }
 
+constexpr int kMaxCluster = 8;
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// sixteen bytes at the address `here` (of this CTA's shared memory) in CTA `rank` of the cluster
+__device__ __forceinline__ float4 peer_float4(uint32_t here, int rank) {
+  float4 r;
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+               : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "r"(here), "r"(rank) : "memory");
+  return r;
+}
+
 // Where eight consecutive keys lie (page_size is a multiple of 8): the first one's rows, and its row of scales; k null: no page of the pool
 struct Octet {
   const uint8_t *k, *v;
@@ -174,6 +186,7 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
   static_assert(kRowsTile * kPitch * 4 <= Rg::kBytes, "a warp's sums take the place of its ring");
   extern __shared__ __align__(16) uint8_t smem[];
   Octet* oct = reinterpret_cast<Octet*>(smem);                                     // [sp.keys / 8]
+  __shared__ float4 sm_part[kRowsTile];
   __shared__ float sm_m[kWarps][kRowsTile], sm_l[kWarps][kRowsTile], sm_r[kWarps][kRowsTile];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -181,9 +194,12 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
   uint8_t* const ring = rings + warp * Rg::kBytes;
   float* const k_factor = reinterpret_cast<float*>(ring + Rg::kStages * Rg::kStage);              // [KS][NB]
   uint16_t* const v_factor = reinterpret_cast<uint16_t*>(k_factor + KS * NB);                     // [NB][KS]
+  // (parts that form a cluster follow one another; otherwise the tiles that read the same keys do)
   int at = blockIdx.x;
-  const int mt = at % n_mt;  at /= n_mt;
-  const int part = at % sp.parts;  at /= sp.parts;
+  const int inner = sp.cluster ? sp.parts : n_mt, outer = sp.cluster ? n_mt : sp.parts;
+  const int at_inner = at % inner;  at /= inner;
+  const int at_outer = at % outer;  at /= outer;
+  const int mt = sp.cluster ? at_outer : at_inner, part = sp.cluster ? at_inner : at_outer;
   const int seq = dm.by_Hkv(at), h = at - seq * dm.Hkv;
 
   pdl_wait();
@@ -197,7 +213,7 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
   const int first_lim = min(pos0 + dm.by_G(row0), s.keys - 1);         // last key that the tile's first row sees
   const int k0 = part * sp.keys;
   const int k1 = min(k0 + sp.keys, min(pos0 + dm.by_G(last_row), s.keys - 1) + 1);
-  if (part > 0 && k0 >= k1) return;
+  if (part > 0 && k0 >= k1 && !sp.cluster) return;
   const int nk = max(k1 - k0, 0);
 
   bool all_there = true;
@@ -643,6 +659,12 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
         }
       }
     }
+    if (sp.cluster) {
+      // (in place: this thread alone reads here)
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(rings) + r * kPitch + col) = sum;
+      if (col == 0) sm_part[r] = make_float4(top, ls, lr, 0.f);
+      continue;
+    }
     if (whole) {
       const float inv = lr > 0.f ? 1.f / lr : (lr == 0.f ? 0.f : lr);      // (NaN stays NaN)
       *reinterpret_cast<uint2*>(O + tok * dm.os[0] + head * dm.os[1] + col) =
@@ -654,6 +676,38 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
       if (col == 0) *reinterpret_cast<float4*>(part_o + sp.parts * all_rows * D + at_row * 4) = make_float4(top, ls, lr, 0.f);
     }
   }
+  if (!sp.cluster) return;
+  // the cluster's sums meet: each CTA finishes some of the rows
+  cluster_sync();
+  for (int r = part + sp.parts * (threadIdx.x / kCols); r < kRowsTile; r += sp.parts * (kWarps * 32 / kCols)) {
+    const int row = row0 + r, col = (threadIdx.x % kCols) * 4;
+    if (row >= rows) break;
+    const uint32_t here = smem_u32(&sm_part[r]), sums = smem_u32(reinterpret_cast<float*>(rings) + r * kPitch + col);
+    float4 ml[kMaxCluster];
+    float top = kNoRef;
+#pragma unroll
+    for (int p = 0; p < kMaxCluster; ++p)
+      if (p < sp.parts) {
+        ml[p] = peer_float4(here, p);
+        top = fmaxf(top, ml[p].x);
+      }
+    float4 sum = make_float4(0, 0, 0, 0);
+    float ls = 0.f, lr = 0.f;
+#pragma unroll
+    for (int p = 0; p < kMaxCluster; ++p)
+      if (p < sp.parts) {
+        const float f = fast_exp2(ml[p].x - top);
+        const float4 x = peer_float4(sums, p);
+        sum.x += f * x.x; sum.y += f * x.y; sum.z += f * x.z; sum.w += f * x.w;
+        ls += f * ml[p].y;
+        lr += f * ml[p].z;
+      }
+    const int t = dm.by_G(row), head = h * dm.G + (row - t * dm.G), tok = s.q0 + t;
+    const float inv = lr > 0.f ? 1.f / lr : (lr == 0.f ? 0.f : lr);
+    *reinterpret_cast<uint2*>(O + tok * dm.os[0] + head * dm.os[1] + col) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+    if (LSE && col == 0) LSE[(int64_t)tok * dm.Hq + head] = ls > 0.f ? (top + log2f(ls)) * 0.69314718055994530942f : (ls == 0.f ? -INFINITY : ls);
+  }
+  cluster_sync();                       // nobody's shared memory goes while it is read
 }
 
 // Joins the parts of every row: a CTA per (token, query head), whose warps share the parts out among them
@@ -670,12 +724,7 @@ k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict_
   const int tok = blockIdx.x / dm.Hq, head = blockIdx.x - tok * dm.Hq;
   pdl_wait();
   pdl_launch_dependents();
-  int lo = 0, hi = dm.n_seq;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu_q[mid] <= tok) lo = mid; else hi = mid;
-  }
-  const CacheSeq s = cache_seq(dm, cu_q, seq_lens, lo);
+  const CacheSeq s = cache_seq(dm, cu_q, seq_lens, find_seq(cu_q, dm.n_seq, tok));
   if (tok < s.q0 || tok - s.q0 >= s.n || s.keys <= sp.keys) return;
   const int last = min(s.len - s.n_all + (tok - s.q0), s.keys - 1);
   const int parts = last < 0 ? 0 : last / sp.keys + 1;
@@ -737,6 +786,15 @@ int rows_of(const CacheDims& dm, const CacheSplit& sp, const void* Q, const int3
   const int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem, true);
   if (rc) return rc;
   PdlLaunch cfg(dim3((unsigned)ctas), kWarps * 32, smem, st, 0);
+  cudaLaunchAttribute attrs[2];
+  if (sp.cluster) {
+    attrs[0] = cfg.attr;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = sp.parts;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.c.attrs = attrs;
+    cfg.c.numAttrs = 2;
+  }
   const cudaError_t e = cudaLaunchKernelEx(&cfg.c, kernel, dm, sp, n_mt, (const uint16_t*)Q, cu_q, seq_lens, table, (const uint8_t*)K,
                                            (const uint8_t*)V, (const uint8_t*)K_scale, (const uint8_t*)V_scale, (uint16_t*)O, LSE,
                                            (float*)workspace, status_word);
@@ -753,7 +811,12 @@ CacheSplit cache_rows_split(const CacheDims& dm) {
   const int64_t want = (dm.max_keys * tiles + 148 * 3 - 1) / (148 * 3);
   CacheSplit sp;
   sp.keys = (int)std::min<int64_t>(std::max<int64_t>((want + 127) / 128 * 128, 256), dm.format == kCacheMx8 ? 1536 : 2048);
+  // Clusters for what is on the device at one time anyway: a CTA without keys keeps its place until its cluster is done.  There, latency
+  // alone counts.
+  const int64_t at_once = 148 * 2;
+  if (dm.max_keys <= kMaxCluster * 128 && tiles * ((dm.max_keys + 127) / 128) <= at_once) sp.keys = 128;
   sp.parts = std::max((dm.max_keys + sp.keys - 1) / sp.keys, 1);
+  sp.cluster = sp.parts > 1 && sp.parts <= kMaxCluster && tiles * sp.parts <= at_once;
   return sp;
 }
 
@@ -775,7 +838,7 @@ int launch_cache_attn_rows(const CacheDims& dm, const CacheSplit& sp, const void
   auto* f = dm.format == kCacheBf16 ? HGA_ROWS(kCacheBf16) : dm.format == kCacheMx8 ? HGA_ROWS(kCacheMx8) : HGA_ROWS(kCacheMx4);
 #undef HGA_ROWS
   const int rc = f(dm, sp, Q, cu_q, seq_lens, table, K, V, K_scale, V_scale, O, LSE, workspace, status_word, st);
-  if (rc || sp.parts == 1) return rc;
+  if (rc || sp.parts == 1 || sp.cluster) return rc;
   return launch_cache_join(dm, sp, cu_q, seq_lens, workspace, O, LSE, st);
 }
 

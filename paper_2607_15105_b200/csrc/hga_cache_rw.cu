@@ -98,12 +98,7 @@ k_cache_write(const CacheDims dm, const uint16_t* __restrict__ K_new, const uint
     if (t < dm.n_tokens && K_new) k[u] = __ldcs(reinterpret_cast<const uint4*>(K_new + t * dm.kns[0] + h * dm.kns[1] + c * 8));
     if (t < dm.n_tokens && V_new) v[u] = __ldcs(reinterpret_cast<const uint4*>(V_new + t * dm.vns[0] + h * dm.vns[1] + c * 8));
   }
-  // the sequence of the first token: the last one that starts at or ahead of it
-  int lo = 0, hi = dm.n_seq;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu_q[mid] <= t0) lo = mid; else hi = mid;
-  }
+  int lo = find_seq(cu_q, dm.n_seq, t0 - (int)(threadIdx.x & 31) / CH);      // of the warp's first row
   bool bad = false;
   int page[kWriteRows], r[kWriteRows];
   CacheSeq s = cache_seq(dm, cu_q, seq_lens, lo);
