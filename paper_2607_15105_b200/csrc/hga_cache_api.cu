@@ -64,7 +64,10 @@ static int resolve_cache(const hga_cache_params* p, CacheDims& dm) {
   return HGA_OK;
 }
 
-static bool few_rows(const CacheDims& dm) { return (int64_t)dm.max_new * dm.G <= 64; }
+// Which kernel: rows of a sequence's (new tokens x query heads of a group) in tiles of 16 that each read the keys again, or in tiles of 128.
+// 16 sequences of up to 32K, 4 key/value heads, us (tiles of 16 / 128): bf16 35 rows 137 / 147, 63 rows 241 / 152; e2m1 35 rows 106 / 235, 63
+// rows 173 / 238, 126 rows - / 235 (converting the keys is most of the work there).
+static bool few_rows(const CacheDims& dm) { return (int64_t)dm.max_new * dm.G <= (dm.format == HGA_CACHE_BF16 ? 48 : 64); }
 static CacheSplit attn_split(const CacheDims& dm) { return few_rows(dm) ? cache_rows_split(dm) : cache_tensor_split(dm); }
 
 }  // namespace hga

@@ -174,6 +174,39 @@ def test_attention(fmt, case):
     assert torch.equal(O.view(torch.int16), again.view(torch.int16))
 
 
+@pytest.mark.parametrize("fmt", ("bf16", "mx4"))
+@pytest.mark.parametrize("n_seq,most", ((40, 90), (600, 90), (40, 3), (1500, 2)))
+def test_many_sequences(fmt, n_seq, most):
+    """sequences without new tokens among them; more than a warp, a block and 32 x 32 of them"""
+    r = np.random.RandomState(n_seq)
+    seqs = [(int(r.choice((0, 0, 1, 2))), int(r.randint(2, 40))) for _ in range(n_seq)]
+    seqs[n_seq // 3], seqs[n_seq - 2], seqs[5] = (most, most + 50), (most - 1, most + 1), (0, 0)
+    pr = T.Problem(seqs, fmt, hq=2, hkv=1, d=64, page=8, seed=21)
+    K, V = pr.randn(pr.n_tokens, 1, 64), pr.randn(pr.n_tokens, 1, 64)
+    binding.hga_cache_write(pr.p, K.cuda(), V.cuda(), pr.d_cu, pr.d_lens, pr.d_table, *pr.cache(), pr.status)
+    values = pr.values("K")
+    for row, pg, slot in pr.new_slots():
+        x = T.f64(K[row, 0])
+        assert np.array_equal(values[pg, 0, slot], x if fmt == "bf16" else T.held(*T.quantise(x[None], fmt), fmt)[0])
+    Q = pr.randn(pr.n_tokens, 2, 64)
+    O, LSE = pr.run_attn(Q.cuda())
+    pr.check_attn(Q, O, LSE)
+    assert int(pr.status.item()) == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_kernels_are_the_ones_meant(fmt):
+    """tiles of 16 rows for few of them, of 128 for more; parts joined in a cluster or by a kernel of its own"""
+    for new, length, hq, rows, tensor in ((1, 100, 8, 1, 0), (1, 700, 8, 1, 0), (1, 9000, 8, 2, 0), (12, 300, 4, 1, 0), (70, 300, 4, 0, 1), (70, 9000, 4, 1, 1)):
+        pr = T.Problem([(new, length)], fmt, hq=hq, hkv=1, d=64, page=64, seed=22)
+        Q = pr.randn(pr.n_tokens, hq, 64).cuda()
+        before = binding.hga_kernel_launch_counts()
+        pr.run_attn(Q)
+        ran = [b - a for a, b in zip(before, binding.hga_kernel_launch_counts())]
+        assert ran[binding.HGA_KERNELS_CACHE_ROWS] == rows and ran[binding.HGA_KERNELS_CACHE_TENSOR] == tensor, (new, length, ran)
+        assert sum(ran) == rows + tensor
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("seqs", ([(4, 2), (3, 0), (2, 300), (6, 5)], [(200, 90), (70, 0), (130, 300)]))
 def test_rows_without_keys(fmt, seqs):
