@@ -9,7 +9,7 @@
 //
 //   warps 0-3, 4-7   softmax and epilogue of M-tile 0 and 1
 //   warps 8, 9       issue the GEMMs of M-tile 0 and 1
-//   warps 10, 11     copy K and V tiles by TMA, a box per page part (quantised pages: as they are, warp 10 alone)
+//   warps 10, 11     copy K and V tiles by TMA, a box per page part (quantised pages: as they are, and their scales)
 //   warps 12-15      bf16 pages: clean the last V tiles; quantised: convert K and V tiles
 //
 // Quantised pages are multiplied as fp16, into which the converter instructions go and which holds e4m3 and e2m1 with their scales
@@ -553,8 +553,10 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
           next();
         }
       }
-    } else if (!kScaled || warp == 10) {
-      // ---------------------------------------------------------------- copies: of K by warp 10, of V by warp 11; quantised: both by 10
+    } else {
+      // ---------------------------------------------------------------- copies: of K by warp 10, of V by warp 11
+      const bool is_v = warp == 11;
+      const CUtensorMap* map = is_v ? &map_v : &map_k;
       const int boxes = kTile / plan.box;
       bool bad = false;
       // lane's box `at` of tile j: its page (a page behind the last one arrives as zeros) and row there
@@ -568,8 +570,6 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         return page;
       };
       if (!kScaled) {
-        const bool is_v = warp == 11;
-        const CUtensorMap* map = is_v ? &map_v : &map_k;
 #pragma unroll 1
         for (int j = 0; j < n_tiles; ++j) {
           const int at_ring = 2 * j + is_v, use = at_ring / NS, slot = at_ring - use * NS;
@@ -587,20 +587,19 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
           __syncwarp();
         }
       } else {
+        uint8_t* dst = sm.raw[is_v];
+        uint64_t* bar = &sm.raw_full[is_v];
+        const uint8_t* all_scales = is_v ? V_scale : K_scale;
 #pragma unroll 1
-        for (int i = 0; i < 2 * n_tiles; ++i) {
-          const int j = i >> 1;
-          const bool is_v = i & 1;
-          uint8_t* dst = sm.raw[i & 1];
-          uint64_t* bar = &sm.raw_full[i & 1];
-          if (!all_wait(&sm.raw_empty[i & 1], ((i >> 1) & 1) ^ 1, abort)) break;
+        for (int j = 0; j < n_tiles; ++j) {
+          if (!all_wait(&sm.raw_empty[is_v], (j & 1) ^ 1, abort)) break;
           if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kRaw + Sm::kRawScales);
           __syncwarp();
           if (lane < boxes) {
             int r;
             const int page = place(j, lane, r);
-            tma_load_5d(dst + lane * plan.box * cache_row_bytes(FMT, D), is_v ? &map_v : &map_k, bar, 0, r, h, page, 0);
-            const uint8_t* scales = (is_v ? V_scale : K_scale) + (((int64_t)page * dm.Hkv + h) * dm.page + r) * (D / 32);
+            tma_load_5d(dst + lane * plan.box * cache_row_bytes(FMT, D), map, bar, 0, r, h, page, 0);
+            const uint8_t* scales = all_scales + (((int64_t)page * dm.Hkv + h) * dm.page + r) * (D / 32);
             bulk_load(dst + Sm::kRaw + lane * plan.box * (D / 32), page < dm.n_pages ? scales : kNoScales, plan.box * (D / 32), bar);
           }
           __syncwarp();
