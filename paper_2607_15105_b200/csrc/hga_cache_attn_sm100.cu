@@ -101,6 +101,25 @@ __device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort));
 }
 
+// 2^x of two numbers x <= 2^20 on the FMA pipe, for a share of the weights: the special-function units take 8 cycles per warp and number, which
+// bounds the softmax.  x = n + f, |f| <= 1/2, n by adding and subtracting 1.5 2^23; 2^f by a polynomial fitted here for least relative error
+// (2.6e-6; weights are rounded to 2^-9 or 2^-12); 2^n from its bits.  Below -127, and for -inf: 0.  NaN stays NaN.
+__device__ __forceinline__ void exp2_by_fma(float& x0, float& x1) {
+  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x0));
+  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x1));
+  const uint64_t x = pack_f32x2(x0, x1), t = add_f32x2(x, pack_f32x2(12582912.f, 12582912.f));
+  const uint64_t n = add_f32x2(t, pack_f32x2(-12582912.f, -12582912.f)), f = fma_f32x2(n, pack_f32x2(-1.f, -1.f), x);
+  uint64_t p = pack_f32x2(0.009570101276040077f, 0.009570101276040077f);
+  p = fma_f32x2(p, f, pack_f32x2(0.05591785907745361f, 0.05591785907745361f));
+  p = fma_f32x2(p, f, pack_f32x2(0.240247443318367f, 0.240247443318367f));
+  p = fma_f32x2(p, f, pack_f32x2(0.6931217908859253f, 0.6931217908859253f));
+  p = fma_f32x2(p, f, pack_f32x2(0.9999992847442627f, 0.9999992847442627f));
+  float t0, t1;
+  unpack_f32x2(t, t0, t1);
+  p = mul_f32x2(p, pack_f32x2(__uint_as_float((__float_as_uint(t0) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t1) << 23) + 0x3f800000u)));
+  unpack_f32x2(p, x0, x1);
+}
+
 __device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7f80u) == 0x7f80u; }
 
 // The unit's place
@@ -346,6 +365,9 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     ok = true;
     auto steps = [&](auto as_f16) {
     constexpr bool kF16 = decltype(as_f16)::value;
+    // One weight in eight by the FMA pipe: chunk of 2048 495 -> 475 us, one in four 485, one in two 507.  Not where a quantised head_dim 128 leaves
+    // too few issue slots (569 -> 580).
+    constexpr bool kByFma = !kScaled || D == 64;
 #pragma unroll 1
     for (int j = 0; j < n; ++j) {
       ok = all_wait(&sm.s_full[x][j & 1], (j >> 1) & 1, abort);
@@ -384,8 +406,12 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
             top[i] = fmaxf(top[i], fmaxf(x0, x1));
             float a0, a1;
             unpack_f32x2(fma_f32x2(pack_f32x2(x0, x1), to_log2_2, neg_m), a0, a1);
-            a0 = fast_exp2(a0);
-            a1 = fast_exp2(a1);
+            if (kByFma && (e & 7) == 5) {
+              exp2_by_fma(a0, a1);
+            } else {
+              a0 = fast_exp2(a0);
+              a1 = fast_exp2(a1);
+            }
             sum2[i] = add_f32x2(sum2[i], pack_f32x2(a0, a1));
             p[e] = kF16 ? pack_f16(a0, a1) : pack_bf16(a0, a1);
           }
