@@ -1,7 +1,7 @@
 // hga_cache_write, hga_cache_read: new tokens into the paged cache, resident ones back as dense bf16.
 //
-// Both are streams: a thread has eight consecutive numbers of one row of K and the same ones of V, so that a warp's accesses are
-// contiguous on the dense side (512 bytes) and, row by row, on the cache's.
+// Both are streams, bound by instructions as much as by bytes.  A thread has eight numbers of either half of a row of K and the same ones of
+// V, and several rows: the lanes of a row access whole sectors on both sides, and where a row lies is worked out once for the four pieces.
 #include "hga_cache.cuh"
 #include "hga_sm100.cuh"
 
@@ -75,9 +75,9 @@ __device__ __forceinline__ void put8(uint4 x, uint8_t* row, uint8_t* scale, int 
   if ((c & 3) == 0) scale[c >> 2] = (uint8_t)s;
 }
 
-// A CTA takes kWriteRows x 2048 / D consecutive tokens of one head, so that it writes whole sectors of scales, and a thread has all its rows in
+// A CTA takes kWriteRows x 4096 / D consecutive tokens of one head, so that it writes whole sectors of scales, and a thread has all its rows in
 // flight at once.
-constexpr int kWriteRows = 2;
+constexpr int kWriteRows = 1;
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(256)
@@ -85,18 +85,23 @@ k_cache_write(const CacheDims dm, const uint16_t* __restrict__ K_new, const uint
               const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table,
               uint8_t* __restrict__ K, uint8_t* __restrict__ V, uint8_t* __restrict__ K_scale, uint8_t* __restrict__ V_scale,
               int32_t* status_word) {
-  constexpr int CH = D / 8, kRows = 256 / CH;   // threads of a row, rows of one access of the CTA
+  constexpr int CH = D / 16, kRows = 256 / CH;  // threads of a row, rows of one access of the CTA
   const int blk = dm.by_Hkv(blockIdx.x), h = blockIdx.x - blk * dm.Hkv;
   const int t0 = blk * (kRows * kWriteRows) + threadIdx.x / CH, c = threadIdx.x % CH;
   pdl_wait();
   pdl_launch_dependents();
-  uint4 k[kWriteRows], v[kWriteRows];
+  uint4 k[kWriteRows][2], v[kWriteRows][2];
 #pragma unroll
   for (int u = 0; u < kWriteRows; ++u) {
     const int64_t t = t0 + u * kRows;
-    k[u] = v[u] = make_uint4(0, 0, 0, 0);
-    if (t < dm.n_tokens && K_new) k[u] = __ldcs(reinterpret_cast<const uint4*>(K_new + t * dm.kns[0] + h * dm.kns[1] + c * 8));
-    if (t < dm.n_tokens && V_new) v[u] = __ldcs(reinterpret_cast<const uint4*>(V_new + t * dm.vns[0] + h * dm.vns[1] + c * 8));
+    const uint16_t* const kr = K_new + t * dm.kns[0] + h * dm.kns[1] + c * 8;
+    const uint16_t* const vr = V_new + t * dm.vns[0] + h * dm.vns[1] + c * 8;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      k[u][i] = v[u][i] = make_uint4(0, 0, 0, 0);
+      if (t < dm.n_tokens && K_new) k[u][i] = __ldcs(reinterpret_cast<const uint4*>(kr + i * (D / 2)));
+      if (t < dm.n_tokens && V_new) v[u][i] = __ldcs(reinterpret_cast<const uint4*>(vr + i * (D / 2)));
+    }
   }
   int lo = find_seq(cu_q, dm.n_seq, t0 - (int)(threadIdx.x & 31) / CH);      // of the warp's first row
   bool bad = false;
@@ -124,8 +129,13 @@ k_cache_write(const CacheDims dm, const uint16_t* __restrict__ K_new, const uint
     const unsigned mask = __ballot_sync(0xffffffffu, here);
     if (here) {
       const int64_t srow = (((int64_t)page[u] * dm.Hkv + h) * dm.page + r[u]) * (D / 32);
-      if (K_new) put8<FMT>(k[u], K + (page[u] * dm.ks[0] + h * dm.ks[1] + r[u] * dm.ks[2]) * kUnit, K_scale + srow, c, mask);
-      if (V_new) put8<FMT>(v[u], V + (page[u] * dm.vs[0] + h * dm.vs[1] + r[u] * dm.vs[2]) * kUnit, V_scale + srow, c, mask);
+      uint8_t* const kr = K + (page[u] * dm.ks[0] + h * dm.ks[1] + r[u] * dm.ks[2]) * kUnit;
+      uint8_t* const vr = V + (page[u] * dm.vs[0] + h * dm.vs[1] + r[u] * dm.vs[2]) * kUnit;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (K_new) put8<FMT>(k[u][i], kr, K_scale + srow, c + i * CH, mask);
+        if (V_new) put8<FMT>(v[u][i], vr, V_scale + srow, c + i * CH, mask);
+      }
     }
     __syncwarp();
   }
@@ -165,7 +175,7 @@ __device__ __forceinline__ uint4 take8(uint32_t x, uint32_t scale) {
   return scaled(y, scale);
 }
 
-constexpr int kReadRows = 4;      // rows a thread has in flight
+constexpr int kReadRows = 2;      // rows a thread has in flight
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(256)
@@ -174,7 +184,8 @@ k_cache_read(const CacheDims dm, int tok_begin, int n, const int32_t* __restrict
              const uint8_t* __restrict__ V_scale, uint16_t* __restrict__ K_out, uint16_t* __restrict__ V_out, int32_t* status_word,
              int blocks_per_head) {
   typedef typename Raw8<FMT>::type Raw;
-  constexpr int CH = D / 8, kRows = 256 / CH;
+  typedef typename ScaleWord<D>::type SW;
+  constexpr int CH = D / 16, kRows = 256 / CH;
   const int bh = blockIdx.x / blocks_per_head, blk = blockIdx.x - bh * blocks_per_head;
   const int i = dm.by_Hkv(bh), h = bh - i * dm.Hkv;
   const int c = threadIdx.x % CH, r0 = blk * (kRows * kReadRows) + threadIdx.x / CH;
@@ -183,37 +194,45 @@ k_cache_read(const CacheDims dm, int tok_begin, int n, const int32_t* __restrict
   pdl_launch_dependents();
   const int len = seq_lens[i];
   bool bad = len < 0 || len > dm.max_keys;
-  const int end = min(len, dm.max_keys) - tok_begin;      // rows of this sequence that are there
-  Raw k[kReadRows], v[kReadRows];
-  uint32_t ks[kReadRows], vs[kReadRows];
+  const int end = min(min(len, dm.max_keys) - tok_begin, n);      // rows of this sequence that are there
+  const uint8_t* const k0 = K + h * dm.ks[1] * kUnit + c * sizeof(Raw);
+  const uint8_t* const v0 = V + h * dm.vs[1] * kUnit + c * sizeof(Raw);
+  Raw k[kReadRows][2], v[kReadRows][2];
+  SW ks[kReadRows], vs[kReadRows];
 #pragma unroll
   for (int u = 0; u < kReadRows; ++u) {
     const int r = r0 + u * kRows;
-    k[u] = Raw{};
-    v[u] = Raw{};
-    ks[u] = vs[u] = 127;
-    if (r < n && r < end) {
+    k[u][0] = k[u][1] = v[u][0] = v[u][1] = Raw{};
+    ks[u] = vs[u] = 0;
+    if (r < end) {
       const int pos = tok_begin + r, e = dm.by_page(pos), pr = pos - e * dm.page;
       const int page = table[i * dm.table_stride + e];
       if (page < 0 || page >= dm.n_pages) { bad = true; continue; }
-      const int64_t srow = (((int64_t)page * dm.Hkv + h) * dm.page + pr) * (D / 32) + (c >> 2);
+      const int64_t srow = (((int64_t)page * dm.Hkv + h) * dm.page + pr) * (D / 32);
+      const uint8_t* const kr = k0 + (page * dm.ks[0] + pr * dm.ks[2]) * kUnit;
+      const uint8_t* const vr = v0 + (page * dm.vs[0] + pr * dm.vs[2]) * kUnit;
       if (K_out) {
-        k[u] = *reinterpret_cast<const Raw*>(K + (page * dm.ks[0] + h * dm.ks[1] + pr * dm.ks[2]) * kUnit + c * sizeof(Raw));
-        if (FMT != kCacheBf16) ks[u] = K_scale[srow];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) k[u][j] = *reinterpret_cast<const Raw*>(kr + j * CH * sizeof(Raw));
+        if (FMT != kCacheBf16) ks[u] = *reinterpret_cast<const SW*>(K_scale + srow);
       }
       if (V_out) {
-        v[u] = *reinterpret_cast<const Raw*>(V + (page * dm.vs[0] + h * dm.vs[1] + pr * dm.vs[2]) * kUnit + c * sizeof(Raw));
-        if (FMT != kCacheBf16) vs[u] = V_scale[srow];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) v[u][j] = *reinterpret_cast<const Raw*>(vr + j * CH * sizeof(Raw));
+        if (FMT != kCacheBf16) vs[u] = *reinterpret_cast<const SW*>(V_scale + srow);
       }
     }
   }
+  int64_t at = i * dm.outs[0] + h * dm.outs[1] + r0 * dm.outs[2] + c * 8;
+  const int sh = 8 * (c >> 2);                    // of this thread's block in the half
 #pragma unroll
-  for (int u = 0; u < kReadRows; ++u) {
-    const int r = r0 + u * kRows;
-    if (r < n && r < end) {
-      const int64_t at = i * dm.outs[0] + h * dm.outs[1] + r * dm.outs[2] + c * 8;
-      if (K_out) *reinterpret_cast<uint4*>(K_out + at) = take8(k[u], ks[u]);
-      if (V_out) *reinterpret_cast<uint4*>(V_out + at) = take8(v[u], vs[u]);
+  for (int u = 0; u < kReadRows; ++u, at += kRows * dm.outs[2]) {
+    if (r0 + u * kRows >= end) break;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int s = sh + j * 4 * (D / 32);
+      if (K_out) *reinterpret_cast<uint4*>(K_out + at + j * (D / 2)) = take8(k[u][j], (ks[u] >> s) & 255u);
+      if (V_out) *reinterpret_cast<uint4*>(V_out + at + j * (D / 2)) = take8(v[u][j], (vs[u] >> s) & 255u);
     }
   }
   if (bad && c == 0) cache_status(status_word, HGA_STATUS_BAD_INDEX);
@@ -222,7 +241,7 @@ k_cache_read(const CacheDims dm, int tok_begin, int n, const int32_t* __restrict
 template <int FMT, int D>
 int write_of(const CacheDims& dm, const void* K_new, const void* V_new, const int32_t* cu_q, const int32_t* seq_lens,
              const int32_t* table, void* K, void* V, void* K_scale, void* V_scale, int32_t* status_word, cudaStream_t st) {
-  constexpr int per = 256 / (D / 8) * kWriteRows;
+  constexpr int per = 256 / (D / 16) * kWriteRows;
   PdlLaunch cfg(dim3((unsigned)((int64_t)((dm.n_tokens + per - 1) / per) * dm.Hkv)), 256, 0, st, 0);
   const cudaError_t e = cudaLaunchKernelEx(&cfg.c, k_cache_write<FMT, D>, dm, (const uint16_t*)K_new, (const uint16_t*)V_new, cu_q,
                                            seq_lens, table, (uint8_t*)K, (uint8_t*)V, (uint8_t*)K_scale, (uint8_t*)V_scale,
@@ -234,7 +253,7 @@ int write_of(const CacheDims& dm, const void* K_new, const void* V_new, const in
 template <int FMT, int D>
 int read_of(const CacheDims& dm, int tok_begin, int n, const int32_t* seq_lens, const int32_t* table, const void* K, const void* V,
             const void* K_scale, const void* V_scale, void* K_out, void* V_out, int32_t* status_word, cudaStream_t st) {
-  constexpr int per = 256 / (D / 8) * kReadRows;
+  constexpr int per = 256 / (D / 16) * kReadRows;
   const int blocks = (n + per - 1) / per;
   PdlLaunch cfg(dim3((unsigned)((int64_t)blocks * dm.n_seq * dm.Hkv)), 256, 0, st, 0);
   const cudaError_t e = cudaLaunchKernelEx(&cfg.c, k_cache_read<FMT, D>, dm, tok_begin, n, seq_lens, table, (const uint8_t*)K,
