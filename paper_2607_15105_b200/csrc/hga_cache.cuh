@@ -118,11 +118,15 @@ int launch_cache_read(const CacheDims& dm, int tok_begin, int tok_end, const int
 // How hga_cache_attn shares out a problem: `keys` consecutive keys (a multiple of 128) go to one CTA, `parts` = what the longest
 // sequence has of these.  Up to eight parts (few rows) form a cluster, whose CTAs join their results through each other's shared memory;
 // otherwise they leave them in the workspace, which a second kernel joins.
+// With `unit` set (chunks of one sequence), only the units of `unit` tokens from number `full` on are shared out, counted from the last and
+// head by head: those that would leave most SMs idle behind the whole ones.
 struct CacheSplit {
   int keys, parts;
   bool cluster;
+  int tokens;               // of the partial results: the first ones
+  int unit, units, full;
   size_t bytes(const CacheDims& dm) const {
-    return parts > 1 && !cluster ? (size_t)parts * dm.n_tokens * dm.Hq * (dm.d + 4) * sizeof(float) : 0;
+    return parts > 1 && !cluster ? (size_t)parts * tokens * dm.Hq * (dm.d + 4) * sizeof(float) : 0;
   }
 };
 CacheSplit cache_rows_split(const CacheDims& dm);

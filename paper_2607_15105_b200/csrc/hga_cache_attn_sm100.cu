@@ -149,8 +149,13 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   // Which unit: the longest first, so that the SMs end at one time, and the heads of a unit one after another.  Units are counted off
   // sequence after sequence, and the late tokens of a sequence see most keys; with several sequences they are ranked by their steps
   // (up to 512; 12 sequences of up to 1000 new tokens, 108 units: 633 us in the order of the sequences, 564 so).
-  int at = blockIdx.x;
-  const int part = at % plan.sp.parts;  at /= plan.sp.parts;
+  int at = blockIdx.x, part = 0;
+  const bool split = plan.sp.parts > 1 && at >= plan.sp.full;
+  if (split) {
+    const int i = at - plan.sp.full;
+    at = plan.sp.full + i / plan.sp.parts;
+    part = i % plan.sp.parts;
+  }
   const int rank = dm.by_Hkv(at), h = at - rank * dm.Hkv;
   if (plan.ranked) {
     int* const first = reinterpret_cast<int*>(sm.ring);        // [n_seq + 1] first unit of a sequence
@@ -258,7 +263,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   const int pos0 = s.len - s.n_all;
   const int n_tok = min(s.n - token0, 2 * plan.tokens);        // of the unit
   const int first_lim = min(pos0 + token0, s.keys - 1), last_lim = min(pos0 + token0 + n_tok - 1, s.keys - 1);
-  const int k0 = part * plan.sp.keys, k1 = min(k0 + plan.sp.keys, last_lim + 1);
+  const int k0 = part * plan.sp.keys, k1 = split ? min(k0 + plan.sp.keys, last_lim + 1) : last_lim + 1;
   if (part > 0 && k0 >= k1) {
     pdl_launch_dependents();
     return;
@@ -454,8 +459,9 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     } while (again());
     if (!*abort && n_tok > x * plan.tokens) {
       tc_fence_after_sync();
-      const bool whole = s.keys <= plan.sp.keys;
-      const int64_t all_rows = (int64_t)dm.n_tokens * dm.Hq, out_row = (int64_t)row * dm.Hq + head;
+      const bool whole = !split || (plan.sp.unit ? last_lim + 1 : s.keys) <= plan.sp.keys;
+      const int64_t all_rows = (int64_t)plan.sp.tokens * dm.Hq, out_row = (int64_t)row * dm.Hq + head;
+      const int64_t part_row = part * all_rows + (int64_t)(plan.sp.unit ? row - s.q0 : row) * dm.Hq + head;
       const float down = f16 ? 1.f / (float)(1 << kLift) : 1.f;                   // (V's lift)
       const float inv = l > 0.f ? (whole ? 1.f / l : 1.f) * down : (l == 0.f ? 0.f : l);      // (NaN stays NaN)
 #pragma unroll 1
@@ -496,7 +502,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
             dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
           }
         } else {
-          uint4* dst = reinterpret_cast<uint4*>(part_o + (part * all_rows + out_row) * D + c);
+          uint4* dst = reinterpret_cast<uint4*>(part_o + part_row * D + c);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             reinterpret_cast<float4*>(dst)[e] = make_float4(__uint_as_float(o[4 * e]) * inv, __uint_as_float(o[4 * e + 1]) * inv,
@@ -505,7 +511,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
       if (real && whole && LSE) LSE[out_row] = l > 0.f ? (m + log2f(l)) * 0.69314718055994530942f : (l == 0.f ? -INFINITY : l);
       if (real && !whole)
-        *reinterpret_cast<float4*>(part_o + plan.sp.parts * all_rows * D + (part * all_rows + out_row) * 4) = make_float4(m, l, l, 0.f);
+        *reinterpret_cast<float4*>(part_o + plan.sp.parts * all_rows * D + part_row * 4) = make_float4(m, l, l, 0.f);
     }
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
@@ -778,13 +784,36 @@ Plan plan_of(const CacheDims& dm) {
   // sum over the sequences of ceil(n / unit) <= tokens / unit + sequences; no sequence has more than max_new
   const int64_t unit = 2 * p.tokens;
   p.units = (int)std::min<int64_t>(dm.n_tokens / unit + std::min(dm.n_seq, dm.n_tokens), dm.n_seq * ((dm.max_new + unit - 1) / unit));
-  // Few units: their keys are shared out, so that the device is full
-  const int64_t ctas = (int64_t)p.units * dm.Hkv;
-  int64_t parts = ctas >= 148 ? 1 : (2 * 148 + ctas - 1) / ctas;
-  const int64_t keys = std::max<int64_t>((dm.max_keys + parts - 1) / parts, 512);
-  p.sp.keys = (int)std::min<int64_t>((keys + kTile - 1) / kTile * kTile, 0x7fffff00);
-  p.sp.parts = (int)std::max<int64_t>((dm.max_keys + p.sp.keys - 1) / p.sp.keys, 1);
+  // Rounds of the device that n units take, whole or in k parts, with what a part and the join add
+  const int n = (int)std::min<int64_t>((int64_t)p.units * dm.Hkv, 0x7fffffff), sms = 148;
+  auto rounds = [&](int64_t n, int k) { return (double)((n * k + sms - 1) / sms) / k + (k > 1 ? 0.04 + 0.01 * k : 0.); };
+  auto best_parts = [&](int64_t n) {
+    int best = 1;
+    for (int k = 2; k <= 32 && dm.max_keys / k >= 512; ++k)
+      if (rounds(n, k) < rounds(n, best) - 0.02) best = k;
+    return best;
+  };
   p.sp.cluster = false;
+  p.sp.tokens = dm.n_tokens;
+  p.sp.unit = p.sp.units = p.sp.full = 0;
+  int k = 1;
+  if (n < sms) {
+    // few units: their keys are shared out, so that the device is full, the more the less even their lengths may be
+    k = dm.n_seq == 1 ? best_parts(n) : (2 * sms + n - 1) / n;
+    if (dm.max_keys / k < 512) k = std::max(dm.max_keys / 512, 1);
+  } else if (dm.n_seq == 1 && n < 8 * sms) {   // the last round's: a chunk of 2048 tokens behind 14K, 256 units: 475 us whole, 430 so
+    const int full = n / sms * sms;
+    k = best_parts(n - full);
+    if (k > 1) {
+      p.sp.unit = (int)unit;
+      p.sp.units = p.units;
+      p.sp.full = full;
+      p.sp.tokens = (int)std::min<int64_t>((int64_t)(p.units - full / dm.Hkv) * unit, dm.n_tokens);
+    }
+  }
+  p.sp.keys = (int)std::min<int64_t>(((int64_t)(dm.max_keys + k - 1) / k + kTile - 1) / kTile * kTile, 0x7fffff00);
+  p.sp.parts = std::max((dm.max_keys + p.sp.keys - 1) / p.sp.keys, 1);
+  if (p.sp.parts == 1) p.sp.unit = p.sp.units = p.sp.full = 0;
   p.ranked = dm.n_seq > 1 && dm.n_seq <= kMaxRanked && p.units <= kMaxRanked && p.sp.parts == 1;
   return p;
 }
@@ -793,7 +822,7 @@ template <int FMT, int D>
 int launch_of(const CacheDims& dm, const Plan& plan, const void* Q, const int32_t* cu_q, const int32_t* seq_lens, const int32_t* table,
               const void* K, const void* V, const void* K_scale, const void* V_scale, void* O, float* LSE, void* workspace,
               int32_t* status_word, cudaStream_t st) {
-  const int64_t ctas = (int64_t)plan.units * dm.Hkv * plan.sp.parts;
+  const int64_t ctas = plan.sp.full + ((int64_t)plan.units * dm.Hkv - plan.sp.full) * plan.sp.parts;
   if (ctas > 0x7fffffff) return HGA_ERR_SHAPE;
   CUtensorMap mk = {}, mv = {};
   int bad;

@@ -624,7 +624,7 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
   }
   const bool any_strange = __syncthreads_or(strange);
   const bool whole = s.keys <= sp.keys;                  // the sequence is one part
-  const int64_t all_rows = (int64_t)dm.n_tokens * dm.Hq;
+  const int64_t all_rows = (int64_t)sp.tokens * dm.Hq;
   constexpr int kCols = D / 4;                           // threads of a row
   for (int r = threadIdx.x / kCols; r < kRowsTile; r += kWarps * 32 / kCols) {
     const int row = row0 + r, col = (threadIdx.x % kCols) * 4;
@@ -710,35 +710,47 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
   cluster_sync();                       // nobody's shared memory goes while it is read
 }
 
-// Joins the parts of every row: a CTA per (token, query head), whose warps share the parts out among them
+// Joins the parts of every (token, query head): W of a CTA's warps share the parts of a row out among them.  Eight where there are many parts
+// of few rows (103 parts of 32 rows: one warp each took 35 us longer), one where there are few of many (4 parts of 28672 rows: eight took
+// 130 us longer).
 constexpr int kJoinWarps = 8;
 
-template <int D>
+template <int D, int W>
 __global__ void __launch_bounds__(kJoinWarps * 32)
 k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens,
              const float* __restrict__ part_o, uint16_t* __restrict__ O, float* __restrict__ LSE) {
   constexpr int N = D / 32;
-  __shared__ float sm_o[kJoinWarps][D], sm_l[kJoinWarps], sm_r[kJoinWarps], sm_m[kJoinWarps];
-  const int64_t all_rows = (int64_t)dm.n_tokens * dm.Hq, row = blockIdx.x;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tok = blockIdx.x / dm.Hq, head = blockIdx.x - tok * dm.Hq;
+  __shared__ float sm_o[W][D], sm_l[W], sm_r[W], sm_m[W];
+  const int64_t all_rows = (int64_t)sp.tokens * dm.Hq;      // of the partial results
+  const int warp = (threadIdx.x >> 5) % W, lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * (kJoinWarps / W) + (threadIdx.x >> 5) / W;
   pdl_wait();
   pdl_launch_dependents();
-  const CacheSeq s = cache_seq(dm, cu_q, seq_lens, find_seq(cu_q, dm.n_seq, tok));
-  if (tok < s.q0 || tok - s.q0 >= s.n || s.keys <= sp.keys) return;
+  if (row >= all_rows) return;
+  const int r_tok = (int)(row / dm.Hq), head = (int)(row - (int64_t)r_tok * dm.Hq);
+  const CacheSeq s = cache_seq(dm, cu_q, seq_lens, sp.unit ? 0 : find_seq(cu_q, dm.n_seq, r_tok));
+  const int tok = sp.unit ? s.q0 + r_tok : r_tok;
+  if (tok < s.q0 || tok - s.q0 >= s.n) return;
+  int keys = s.keys;                    // that what was written as one was decided by
+  if (sp.unit) {
+    const int u = r_tok / sp.unit;
+    if ((sp.units - 1 - u) * dm.Hkv + dm.by_G(head) < sp.full) return;
+    keys = min(s.len - s.n_all + min((u + 1) * sp.unit, s.n), s.keys);
+  }
+  if (keys <= sp.keys) return;
   const int last = min(s.len - s.n_all + (tok - s.q0), s.keys - 1);
   const int parts = last < 0 ? 0 : last / sp.keys + 1;
   const float4* ml = reinterpret_cast<const float4*>(part_o + sp.parts * all_rows * D);
   // each warp against the largest reference of its own parts
   float top = kNoRef;
-  for (int i = warp + kJoinWarps * lane; i < parts; i += kJoinWarps * 32) top = fmaxf(top, ml[i * all_rows + row].x);
+  for (int i = warp + W * lane; i < parts; i += W * 32) top = fmaxf(top, ml[i * all_rows + row].x);
 #pragma unroll
   for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
   float sum[N], ls = 0.f, lr = 0.f;
 #pragma unroll
   for (int e = 0; e < N; ++e) sum[e] = 0.f;
 #pragma unroll 4
-  for (int i = warp; i < parts; i += kJoinWarps) {
+  for (int i = warp; i < parts; i += W) {
     const float4 x = ml[i * all_rows + row];
     const float f = fast_exp2(x.x - top);
     ls += f * x.y;
@@ -751,6 +763,15 @@ k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict_
       sum[e + 1] += f * y.y;
     }
   }
+  uint16_t* const out = O + tok * dm.os[0] + head * dm.os[1];
+  float* const lse = LSE ? LSE + (int64_t)tok * dm.Hq + head : nullptr;
+  if (W == 1) {
+    const float inv = lr > 0.f ? 1.f / lr : (lr == 0.f ? 0.f : lr);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(out + lane * N + e) = pack_bf16(sum[e] * inv, sum[e + 1] * inv);
+    if (lse && lane == 0) *lse = ls > 0.f ? (top + log2f(ls)) * 0.69314718055994530942f : (ls == 0.f ? -INFINITY : ls);
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < N; ++e) sm_o[warp][lane * N + e] = sum[e];
   if (lane == 0) { sm_m[warp] = top; sm_l[warp] = ls; sm_r[warp] = lr; }
@@ -758,11 +779,11 @@ k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict_
   if (threadIdx.x >= D / 2) return;
   top = sm_m[0];
 #pragma unroll
-  for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, sm_m[w]);
+  for (int w = 1; w < W; ++w) top = fmaxf(top, sm_m[w]);
   float a = 0.f, b = 0.f;
   ls = lr = 0.f;
 #pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) {
+  for (int w = 0; w < W; ++w) {
     const float f = fast_exp2(sm_m[w] - top);
     a += f * sm_o[w][2 * threadIdx.x];
     b += f * sm_o[w][2 * threadIdx.x + 1];
@@ -770,8 +791,8 @@ k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict_
     lr += f * sm_r[w];
   }
   const float inv = lr > 0.f ? 1.f / lr : (lr == 0.f ? 0.f : lr);
-  *reinterpret_cast<uint32_t*>(O + tok * dm.os[0] + head * dm.os[1] + 2 * threadIdx.x) = pack_bf16(a * inv, b * inv);
-  if (LSE && threadIdx.x == 0) LSE[row] = ls > 0.f ? (top + log2f(ls)) * 0.69314718055994530942f : (ls == 0.f ? -INFINITY : ls);
+  *reinterpret_cast<uint32_t*>(out + 2 * threadIdx.x) = pack_bf16(a * inv, b * inv);
+  if (lse && threadIdx.x == 0) *lse = ls > 0.f ? (top + log2f(ls)) * 0.69314718055994530942f : (ls == 0.f ? -INFINITY : ls);
 }
 
 template <int FMT, int D, int NT>
@@ -817,15 +838,18 @@ CacheSplit cache_rows_split(const CacheDims& dm) {
   if (dm.max_keys <= kMaxCluster * 128 && tiles * ((dm.max_keys + 127) / 128) <= at_once) sp.keys = 128;
   sp.parts = std::max((dm.max_keys + sp.keys - 1) / sp.keys, 1);
   sp.cluster = sp.parts > 1 && sp.parts <= kMaxCluster && tiles * sp.parts <= at_once;
+  sp.tokens = dm.n_tokens;
+  sp.unit = sp.units = sp.full = 0;
   return sp;
 }
 
 int launch_cache_join(const CacheDims& dm, const CacheSplit& sp, const int32_t* cu_q, const int32_t* seq_lens, const void* workspace,
                       void* O, float* LSE, cudaStream_t st) {
-  const int64_t rows = (int64_t)dm.n_tokens * dm.Hq;
-  PdlLaunch cfg(dim3((unsigned)rows), kJoinWarps * 32, 0, st, 0);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg.c, dm.d == 128 ? k_cache_join<128> : k_cache_join<64>, dm, sp, cu_q, seq_lens,
-                                           (const float*)workspace, (uint16_t*)O, LSE);
+  const int64_t rows = (int64_t)sp.tokens * dm.Hq;
+  const bool many = sp.parts > 16 || rows < 148 * 8;
+  auto* kernel = many ? (dm.d == 128 ? k_cache_join<128, kJoinWarps> : k_cache_join<64, kJoinWarps>) : (dm.d == 128 ? k_cache_join<128, 1> : k_cache_join<64, 1>);
+  PdlLaunch cfg(dim3((unsigned)(many ? rows : (rows + kJoinWarps - 1) / kJoinWarps)), kJoinWarps * 32, 0, st, 0);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg.c, kernel, dm, sp, cu_q, seq_lens, (const float*)workspace, (uint16_t*)O, LSE);
   count_launch(HGA_KERNELS_CACHE_ROWS);
   return record_cuda(e);
 }
