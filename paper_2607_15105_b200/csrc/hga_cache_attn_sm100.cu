@@ -145,6 +145,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abort = &sm.abort;
 
+  if ((warp == 10 || warp == 11) && lane == 0) prefetch_tensormap(warp == 11 ? &map_v : &map_k);
   pdl_wait();
   // Which unit: the longest first, so that the SMs end at one time, and the heads of a unit one after another.  Units are counted off
   // sequence after sequence, and the late tokens of a sequence see most keys; with several sequences they are ranked by their steps
@@ -283,16 +284,28 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   // fp16: scales are 2^(code - 127 + kLift), in range from 2^-14 to 2^kTop
   constexpr int kLift = FMT == kCacheMx8 ? 4 : 2, kTop = FMT == kCacheMx8 ? 7 : 13;
   auto load_q = [&](bool f16) {
-    for (int i = tid; i < 2 * kTile * C; i += kThreads) {
-      const int row = i / C, c = i % C, x = row / kTile, r = row % kTile;
-      const int t = dm.by_G(r), tok = x * plan.tokens + t;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (t < plan.tokens && tok < n_tok)
-        v = *reinterpret_cast<const uint4*>(Q + (s.q0 + token0 + tok) * dm.qs[0] + (h * dm.G + r - t * dm.G) * dm.qs[1] + c * 8);
-      if (kScaled) {
-        if (f16) {
+    if (warp == 10 || warp == 11) return;      // (they copy)
+    constexpr int kLoaders = kThreads - 64, kAll = 2 * kTile * C, kAtOnce = (kAll + kLoaders - 1) / kLoaders;      // all of a thread's
+    static_assert(kAtOnce <= 10, "registers");
+    const int first = warp < 10 ? tid : tid - 64;
+#pragma unroll 1
+    for (int base = first; base < kAll; base += kLoaders * kAtOnce) {
+      uint4 v[kAtOnce];
+#pragma unroll
+      for (int b = 0; b < kAtOnce; ++b) {
+        const int i = base + b * kLoaders, row = i / C, c = i % C, x = row / kTile, r = row % kTile;
+        const int t = dm.by_G(r), tok = x * plan.tokens + t;
+        v[b] = make_uint4(0, 0, 0, 0);
+        if (i < kAll && t < plan.tokens && tok < n_tok)
+          v[b] = *reinterpret_cast<const uint4*>(Q + (s.q0 + token0 + tok) * dm.qs[0] + (h * dm.G + r - t * dm.G) * dm.qs[1] + c * 8);
+      }
+#pragma unroll
+      for (int b = 0; b < kAtOnce; ++b) {
+        const int i = base + b * kLoaders, row = i / C, c = i % C, x = row / kTile, r = row % kTile;
+        if (i >= kAll) break;                  // (a whole warp)
+        if (kScaled && f16) {
           // the row's largest to 2^14 .. 2^15, by a power of two that fp32 holds (and its inverse)
-          uint32_t* w = &v.x;
+          uint32_t* w = &v[b].x;
           uint32_t big = 0;
 #pragma unroll
           for (int k = 0; k < 4; ++k) big = max(big, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
@@ -304,16 +317,67 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
           for (int k = 0; k < 4; ++k) w[k] = pack_f16(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xffff0000u) * f);
         }
+        *reinterpret_cast<uint4*>(sm.q[x] + piece<D>(r, c)) = v[b];
       }
-      *reinterpret_cast<uint4*>(sm.q[x] + piece<D>(r, c)) = v;
     }
     fence_proxy_async_smem();
   };
-  load_q(kScaled);
+  // first tile with keys hidden from the unit's first row
+  const int first_dirty = max(first_lim + 1 - k0, 0) / kTile;
+  // Copies of tile j: of K by warp 10, of V by warp 11.  False: a wait ran out.
+  bool bad_page = false;
+  auto copy_tile = [&](int j) {
+    const bool is_v = warp == 11;
+    const CUtensorMap* map = is_v ? &map_v : &map_k;
+    const int boxes = kTile / plan.box;
+    // lane's box `at`: its page (a page behind the last one arrives as zeros) and row there
+    auto place = [&](int at, int& r) {
+      const int key = k0 + j * kTile + at * plan.box;
+      r = 0;
+      if (key >= k1) return dm.n_pages;
+      const int e = dm.by_page(key), page = table[seq * dm.table_stride + e];
+      if (page < 0 || page >= dm.n_pages) { bad_page = true; return dm.n_pages; }
+      r = key - e * dm.page;
+      return page;
+    };
+    if (!kScaled) {
+      const int at_ring = 2 * j + is_v, use = at_ring / NS, slot = at_ring - use * NS;
+      if (!all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) return false;
+      uint64_t* bar = is_v && j >= first_dirty ? &sm.raw_full[slot] : &sm.full[slot];
+      if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kTileBytes);
+      else if (lane < 4 && bar == &sm.full[slot]) mbar_arrive(bar);
+      __syncwarp();
+      if (lane < boxes * (D / 64)) {
+        const int box = lane % boxes, panel = lane / boxes;
+        int r;
+        const int page = place(box, r);
+        tma_load_5d(sm.ring[slot] + panel * (kTile * 128) + box * plan.box * 128, map, bar, 0, r, panel, h, page);
+      }
+    } else {
+      uint8_t* dst = sm.raw[is_v];
+      uint64_t* bar = &sm.raw_full[is_v];
+      if (!all_wait(&sm.raw_empty[is_v], (j & 1) ^ 1, abort)) return false;
+      if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kRaw + Sm::kRawScales);
+      __syncwarp();
+      if (lane < boxes) {
+        int r;
+        const int page = place(lane, r);
+        tma_load_5d(dst + lane * plan.box * cache_row_bytes(FMT, D), map, bar, 0, r, h, page, 0);
+        const uint8_t* scales = (is_v ? V_scale : K_scale) + (((int64_t)page * dm.Hkv + h) * dm.page + r) * (D / 32);
+        bulk_load(dst + Sm::kRaw + lane * plan.box * (D / 32), page < dm.n_pages ? scales : kNoScales, plan.box * (D / 32), bar);
+      }
+    }
+    __syncwarp();
+    return true;
+  };
   if (warp == 8) {
     tmem_alloc(&sm.tmem_base, kTmemCols);
     tmem_relinquish();
+    __syncwarp();
   }
+  // (the first tiles are on their way while Q is fetched)
+  if ((warp == 10 || warp == 11) && n_tiles > 0) copy_tile(0);
+  load_q(kScaled);
   __syncwarp();
   tc_fence_before_sync();
   __syncthreads();
@@ -345,8 +409,6 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __syncthreads();
     return true;
   };
-  // first tile with keys hidden from the unit's first row
-  const int first_dirty = max(first_lim + 1 - k0, 0) / kTile;
 
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax
@@ -464,6 +526,11 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const int64_t part_row = part * all_rows + (int64_t)(plan.sp.unit ? row - s.q0 : row) * dm.Hq + head;
       const float down = f16 ? 1.f / (float)(1 << kLift) : 1.f;                   // (V's lift)
       const float inv = l > 0.f ? (whole ? 1.f / l : 1.f) * down : (l == 0.f ? 0.f : l);      // (NaN stays NaN)
+      // Rows pass through shared memory (every copy and GEMM is done), so that a warp stores them piece after piece: a row per lane instead
+      // took three times as long.
+      constexpr int kPitch = D * 4 + 16;
+      static_assert(8 * 32 * kPitch <= (int)(sizeof(sm.q) + sizeof(sm.ring)), "the rows of eight warps");
+      uint8_t* const mine = sm.q[0] + warp * (32 * kPitch);
 #pragma unroll 1
       for (int c = 0; c < D; c += 32) {
         uint32_t o[32];
@@ -475,8 +542,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0;
         }
-        if (!real) continue;
-        if (sm.strange) {
+        if (sm.strange && real) {
           const int end = min(lim + 1, k1);
           for (int key = max(first_lim + 1, k0); key < end; ++key) {
             const int e0 = dm.by_page(key), pr = key - e0 * dm.page, page = table[seq * dm.table_stride + e0];
@@ -492,22 +558,31 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
           }
         }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
         if (whole) {
-          uint4* dst = reinterpret_cast<uint4*>(O + row * dm.os[0] + head * dm.os[1] + c);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = pack_bf16(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
-            dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int k = 0; k < 4; ++k) w[k] = pack_bf16(__uint_as_float(o[8 * e + 2 * k]), __uint_as_float(o[8 * e + 2 * k + 1]));
+            *reinterpret_cast<uint4*>(mine + lane * kPitch + c * 2 + e * 16) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         } else {
-          uint4* dst = reinterpret_cast<uint4*>(part_o + part_row * D + c);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            reinterpret_cast<float4*>(dst)[e] = make_float4(__uint_as_float(o[4 * e]) * inv, __uint_as_float(o[4 * e + 1]) * inv,
-                                                            __uint_as_float(o[4 * e + 2]) * inv, __uint_as_float(o[4 * e + 3]) * inv);
+            *reinterpret_cast<uint4*>(mine + lane * kPitch + c * 4 + e * 16) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
         }
+      }
+      __syncwarp();
+      const int64_t to = !real ? -1 : whole ? (row * dm.os[0] + head * dm.os[1]) * 2 : part_row * (D * 4);      // bytes
+      uint8_t* const out = whole ? reinterpret_cast<uint8_t*>(O) : reinterpret_cast<uint8_t*>(part_o);
+      const int pieces = whole ? D / 8 : D / 4;           // of a row
+#pragma unroll 4
+      for (int i = lane; i < 32 * pieces; i += 32) {
+        const int64_t at_row = __shfl_sync(0xffffffffu, to, i / pieces);
+        if (at_row >= 0)
+          *reinterpret_cast<uint4*>(out + at_row + i % pieces * 16) = *reinterpret_cast<const uint4*>(mine + i / pieces * kPitch + i % pieces * 16);
       }
       if (real && whole && LSE) LSE[out_row] = l > 0.f ? (m + log2f(l)) * 0.69314718055994530942f : (l == 0.f ? -INFINITY : l);
       if (real && !whole)
@@ -586,58 +661,10 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
       }
     } else {
-      // ---------------------------------------------------------------- copies: of K by warp 10, of V by warp 11
-      const bool is_v = warp == 11;
-      const CUtensorMap* map = is_v ? &map_v : &map_k;
-      const int boxes = kTile / plan.box;
-      bool bad = false;
-      // lane's box `at` of tile j: its page (a page behind the last one arrives as zeros) and row there
-      auto place = [&](int j, int at, int& r) {
-        const int key = k0 + j * kTile + at * plan.box;
-        r = 0;
-        if (key >= k1) return dm.n_pages;
-        const int e = dm.by_page(key), page = table[seq * dm.table_stride + e];
-        if (page < 0 || page >= dm.n_pages) { bad = true; return dm.n_pages; }
-        r = key - e * dm.page;
-        return page;
-      };
-      if (!kScaled) {
-#pragma unroll 1
-        for (int j = 0; j < n_tiles; ++j) {
-          const int at_ring = 2 * j + is_v, use = at_ring / NS, slot = at_ring - use * NS;
-          if (!all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
-          uint64_t* bar = is_v && j >= first_dirty ? &sm.raw_full[slot] : &sm.full[slot];
-          if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kTileBytes);
-          else if (lane < 4 && bar == &sm.full[slot]) mbar_arrive(bar);
-          __syncwarp();
-          if (lane < boxes * (D / 64)) {
-            const int box = lane % boxes, panel = lane / boxes;
-            int r;
-            const int page = place(j, box, r);
-            tma_load_5d(sm.ring[slot] + panel * (kTile * 128) + box * plan.box * 128, map, bar, 0, r, panel, h, page);
-          }
-          __syncwarp();
-        }
-      } else {
-        uint8_t* dst = sm.raw[is_v];
-        uint64_t* bar = &sm.raw_full[is_v];
-        const uint8_t* all_scales = is_v ? V_scale : K_scale;
-#pragma unroll 1
-        for (int j = 0; j < n_tiles; ++j) {
-          if (!all_wait(&sm.raw_empty[is_v], (j & 1) ^ 1, abort)) break;
-          if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kRaw + Sm::kRawScales);
-          __syncwarp();
-          if (lane < boxes) {
-            int r;
-            const int page = place(j, lane, r);
-            tma_load_5d(dst + lane * plan.box * cache_row_bytes(FMT, D), map, bar, 0, r, h, page, 0);
-            const uint8_t* scales = all_scales + (((int64_t)page * dm.Hkv + h) * dm.page + r) * (D / 32);
-            bulk_load(dst + Sm::kRaw + lane * plan.box * (D / 32), page < dm.n_pages ? scales : kNoScales, plan.box * (D / 32), bar);
-          }
-          __syncwarp();
-        }
-      }
-      if (bad) cache_status(status_word, HGA_STATUS_BAD_INDEX);
+      // ---------------------------------------------------------------- copies (tile 0 went ahead)
+      for (int j = f16 == kScaled ? 1 : 0; j < n_tiles; ++j)
+        if (!copy_tile(j)) break;
+      if (bad_page) cache_status(status_word, HGA_STATUS_BAD_INDEX);
       if (*abort && lane == 0) {
         // giving up: give the copies still in flight time to land before shared memory is released
         for (int it = 0; it < 64; ++it) __nanosleep(1000);
@@ -784,13 +811,14 @@ Plan plan_of(const CacheDims& dm) {
   // sum over the sequences of ceil(n / unit) <= tokens / unit + sequences; no sequence has more than max_new
   const int64_t unit = 2 * p.tokens;
   p.units = (int)std::min<int64_t>(dm.n_tokens / unit + std::min(dm.n_seq, dm.n_tokens), dm.n_seq * ((dm.max_new + unit - 1) / unit));
-  // Rounds of the device that n units take, whole or in k parts, with what a part and the join add
+  // What n units take, whole or in k parts, in steps of 64 keys: rounds of the device, a CTA's set-up and end (16 steps' time), the join
   const int n = (int)std::min<int64_t>((int64_t)p.units * dm.Hkv, 0x7fffffff), sms = 148;
-  auto rounds = [&](int64_t n, int k) { return (double)((n * k + sms - 1) / sms) / k + (k > 1 ? 0.04 + 0.01 * k : 0.); };
+  const double steps = dm.max_keys / 64.;
+  auto cost = [&](int64_t n, int k) { return (double)((n * k + sms - 1) / sms) * (steps / k + 16) + (k > 1 ? 25 + 2 * k : 0); };
   auto best_parts = [&](int64_t n) {
     int best = 1;
-    for (int k = 2; k <= 32 && dm.max_keys / k >= 512; ++k)
-      if (rounds(n, k) < rounds(n, best) - 0.02) best = k;
+    for (int k = 2; k <= 64 && dm.max_keys / k >= 512; ++k)
+      if (cost(n, k) < cost(n, best)) best = k;
     return best;
   };
   p.sp.cluster = false;
@@ -801,9 +829,12 @@ Plan plan_of(const CacheDims& dm) {
     // few units: their keys are shared out, so that the device is full, the more the less even their lengths may be
     k = dm.n_seq == 1 ? best_parts(n) : (2 * sms + n - 1) / n;
     if (dm.max_keys / k < 512) k = std::max(dm.max_keys / 512, 1);
-  } else if (dm.n_seq == 1 && n < 8 * sms) {   // the last round's: a chunk of 2048 tokens behind 14K, 256 units: 475 us whole, 430 so
+  } else if (dm.n_seq == 1 && n % sms) {
+    // the last round's, where that takes a tenth off: 1408 tokens behind 15K, 176 units: 467 us whole, 328 so (256 units, whose last round
+    // is fuller: 473 whole, 504 so)
     const int full = n / sms * sms;
     k = best_parts(n - full);
+    if (cost(n - full, 1) - cost(n - full, k) < 0.1 * cost(n, 1)) k = 1;
     if (k > 1) {
       p.sp.unit = (int)unit;
       p.sp.units = p.units;
