@@ -379,9 +379,16 @@ def hga_cache_workspace_bytes(p: HgaCacheParams) -> int:
     return n.value
 
 
+def _check_device(call, t):
+    """The pool lies on the current device, whose stream the call goes to."""
+    if isinstance(t, torch.Tensor) and t.get_device() != torch.cuda.current_device():
+        raise ValueError("%s: the cache is on %s, the current device is cuda:%d" % (call, t.device, torch.cuda.current_device()))
+
+
 def hga_cache_write(p, K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale=None, V_scale=None, status_word=None,
                     stream=None):
     """Keys and values of the new tokens into the paged cache (see hga.h)."""
+    _check_device("hga_cache_write", V_cache if K_cache is None else K_cache)
     _check("hga_cache_write", lib().hga_cache_write(
         C.byref(p), _ptr(K_new), _ptr(V_new), _ptr(cu_q), _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache),
         _ptr(K_scale), _ptr(V_scale), _ptr(status_word), _stream(stream)))
@@ -390,6 +397,7 @@ def hga_cache_write(p, K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cac
 def hga_cache_read(p, tok_begin, tok_end, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, K_out, V_out, status_word=None,
                    stream=None):
     """Resident tokens [tok_begin, tok_end) of every sequence as dense bf16 (see hga.h)."""
+    _check_device("hga_cache_read", V_cache if K_cache is None else K_cache)
     _check("hga_cache_read", lib().hga_cache_read(
         C.byref(p), tok_begin, tok_end, _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale),
         _ptr(K_out), _ptr(V_out), _ptr(status_word), _stream(stream)))
@@ -398,6 +406,7 @@ def hga_cache_read(p, tok_begin, tok_end, seq_lens, block_table, K_cache, V_cach
 def hga_cache_attn(p, Q, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, O, LSE=None, workspace=None,
                    status_word=None, stream=None):
     """Exact attention of the new tokens over the paged cache (see hga.h)."""
+    _check_device("hga_cache_attn", K_cache)
     _check("hga_cache_attn", lib().hga_cache_attn(
         C.byref(p), _ptr(Q), _ptr(cu_q), _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale),
         _ptr(O), _ptr(LSE), _ptr(workspace), _nbytes(workspace), _ptr(status_word), _stream(stream)))

@@ -27,6 +27,9 @@ __device__ __forceinline__ void cache_status(int32_t* status_word, int bits) {
   if (status_word) atomicOr(status_word, bits);
 }
 
+// (The kernels' pointers are not __restrict__: what only such pointers read counts as never written, and the compiler may load it ahead of
+// griddepcontrol.wait, when the call before, which writes the pool, is still at work.)
+
 // The new tokens of sequence i and its resident length, held to the limits; `bad`: they had to be
 struct CacheSeq {
   int q0, n;          // first row of the packed tensors, new tokens

@@ -134,10 +134,10 @@ struct Unit {
 template <int FMT, int D>
 __global__ void __launch_bounds__(kThreads, 1)
 k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                   const CacheDims dm, const Plan plan, const uint16_t* __restrict__ Q, const int32_t* __restrict__ cu_q,
-                   const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table, const uint8_t* __restrict__ K,
-                   const uint8_t* __restrict__ V, const uint8_t* __restrict__ K_scale, const uint8_t* __restrict__ V_scale,
-                   uint16_t* __restrict__ O, float* __restrict__ LSE, float* __restrict__ part_o, int32_t* status_word) {
+                   const CacheDims dm, const Plan plan, const uint16_t* Q, const int32_t* cu_q,
+                   const int32_t* seq_lens, const int32_t* table, const uint8_t* K,
+                   const uint8_t* V, const uint8_t* K_scale, const uint8_t* V_scale,
+                   uint16_t* O, float* LSE, float* part_o, int32_t* status_word) {
   typedef Smem<FMT, D> Sm;
   constexpr int NS = Sm::kSlots;
   extern __shared__ uint8_t raw[];

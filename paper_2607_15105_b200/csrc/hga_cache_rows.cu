@@ -172,10 +172,10 @@ __device__ float strange_value(const uint8_t* row, const uint8_t* scale, int e) 
 
 template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(kWarps * 32, FMT == kCacheMx4 && NT == 1 ? 4 : 3)
-k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* __restrict__ Q, const int32_t* __restrict__ cu_q,
-             const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table, const uint8_t* __restrict__ K,
-             const uint8_t* __restrict__ V, const uint8_t* __restrict__ K_scale, const uint8_t* __restrict__ V_scale,
-             uint16_t* __restrict__ O, float* __restrict__ LSE, float* __restrict__ part_o, int32_t* status_word) {
+k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* Q, const int32_t* cu_q,
+             const int32_t* seq_lens, const int32_t* table, const uint8_t* K,
+             const uint8_t* V, const uint8_t* K_scale, const uint8_t* V_scale,
+             uint16_t* O, float* LSE, float* part_o, int32_t* status_word) {
   typedef Ring<FMT, D> Rg;
   constexpr int kRowsTile = 8 * NT, KS = Rg::KS, SUB = KS / 16, NB = Rg::NB;
   constexpr int kUnit = FMT == kCacheBf16 ? 2 : 1;
@@ -717,8 +717,8 @@ constexpr int kJoinWarps = 8;
 
 template <int D, int W>
 __global__ void __launch_bounds__(kJoinWarps * 32)
-k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens,
-             const float* __restrict__ part_o, uint16_t* __restrict__ O, float* __restrict__ LSE) {
+k_cache_join(const CacheDims dm, const CacheSplit sp, const int32_t* cu_q, const int32_t* seq_lens,
+             const float* part_o, uint16_t* O, float* LSE) {
   constexpr int N = D / 32;
   __shared__ float sm_o[W][D], sm_l[W], sm_r[W], sm_m[W];
   const int64_t all_rows = (int64_t)sp.tokens * dm.Hq;      // of the partial results

@@ -81,9 +81,9 @@ constexpr int kWriteRows = 1;
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(256)
-k_cache_write(const CacheDims dm, const uint16_t* __restrict__ K_new, const uint16_t* __restrict__ V_new,
-              const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table,
-              uint8_t* __restrict__ K, uint8_t* __restrict__ V, uint8_t* __restrict__ K_scale, uint8_t* __restrict__ V_scale,
+k_cache_write(const CacheDims dm, const uint16_t* K_new, const uint16_t* V_new,
+              const int32_t* cu_q, const int32_t* seq_lens, const int32_t* table,
+              uint8_t* K, uint8_t* V, uint8_t* K_scale, uint8_t* V_scale,
               int32_t* status_word) {
   constexpr int CH = D / 16, kRows = 256 / CH;  // threads of a row, rows of one access of the CTA
   const int blk = dm.by_Hkv(blockIdx.x), h = blockIdx.x - blk * dm.Hkv;
@@ -179,9 +179,9 @@ constexpr int kReadRows = 2;      // rows a thread has in flight
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(256)
-k_cache_read(const CacheDims dm, int tok_begin, int n, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ table,
-             const uint8_t* __restrict__ K, const uint8_t* __restrict__ V, const uint8_t* __restrict__ K_scale,
-             const uint8_t* __restrict__ V_scale, uint16_t* __restrict__ K_out, uint16_t* __restrict__ V_out, int32_t* status_word,
+k_cache_read(const CacheDims dm, int tok_begin, int n, const int32_t* seq_lens, const int32_t* table,
+             const uint8_t* K, const uint8_t* V, const uint8_t* K_scale,
+             const uint8_t* V_scale, uint16_t* K_out, uint16_t* V_out, int32_t* status_word,
              int blocks_per_head) {
   typedef typename Raw8<FMT>::type Raw;
   typedef typename ScaleWord<D>::type SW;

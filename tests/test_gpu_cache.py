@@ -422,6 +422,47 @@ def test_two_streams_with_workspaces_of_their_own():
         pr.check_attn(q, O, LSE)
 
 
+def test_a_pool_that_is_not_on_the_current_device_is_refused():
+    pr = T.Problem([(1, 9)], "bf16", hq=1, hkv=1, d=64, seed=23, device="cpu")
+    with pytest.raises(ValueError, match="current device"):
+        pr.run_attn(pr.randn(1, 1, 64))
+    with pytest.raises(ValueError, match="current device"):
+        binding.hga_cache_write(pr.p, None, pr.V_values, pr.d_cu, pr.d_lens, pr.d_table, None, pr.V)
+    with pytest.raises(ValueError, match="current device"):
+        binding.hga_cache_read(pr.p, 0, 9, pr.d_lens, pr.d_table, pr.K, None, None, None, pr.K_values, None)
+
+
+def test_writes_are_seen_by_the_calls_behind_them():
+    """write, read and attention one straight behind the other, with other contents every time: the kernels start before the one ahead has ended"""
+    for fmt in FMTS:
+        pr = T.Problem([(1, 300)] * 8, fmt, hq=4, hkv=2, d=128, page=16, seed=24)
+        n = 20
+        K, V = pr.randn(n, 8, 2, 128).cuda(), pr.randn(n, 8, 2, 128).cuda()
+        Q = pr.randn(8, 4, 128)
+        Qd, ws = Q.cuda(), pr.workspace()
+        O = torch.zeros(n, 8, 4, 128, dtype=torch.bfloat16, device="cuda")
+        out = torch.zeros(n, 8, 2, 300, 128, dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        for i in range(n):
+            binding.hga_cache_write(pr.p, K[i], V[i], pr.d_cu, pr.d_lens, pr.d_table, *pr.cache(), pr.status)
+            binding.hga_cache_attn(pr.p, Qd, pr.d_cu, pr.d_lens, pr.d_table, *pr.cache(), O[i], None, ws, pr.status)
+            binding.hga_cache_write(pr.p, None, K[n - 1 - i], pr.d_cu, pr.d_lens, pr.d_table, None, pr.V, None, pr.V_scale, pr.status)
+            binding.hga_cache_read(pr.p, 0, 300, pr.d_lens, pr.d_table, None, pr.V, None, pr.V_scale, None, out[i], pr.status)
+        torch.cuda.synchronize()
+        for i in range(n):
+            x = T.f64(K[n - 1 - i])
+            want = x if fmt == "bf16" else T.held(*T.quantise(x, fmt), fmt)
+            assert np.array_equal(T.f64(out[i])[:, :, 299], want)
+        again = torch.zeros_like(O)
+        for i in range(n):
+            binding.hga_cache_write(pr.p, K[i], V[i], pr.d_cu, pr.d_lens, pr.d_table, *pr.cache(), pr.status)
+            torch.cuda.synchronize()
+            binding.hga_cache_attn(pr.p, Qd, pr.d_cu, pr.d_lens, pr.d_table, *pr.cache(), again[i], None, ws, pr.status)
+            torch.cuda.synchronize()
+        assert torch.equal(O.view(torch.int16), again.view(torch.int16))
+        pr.check_attn(Q, again[n - 1], None)
+
+
 def test_offsets_beyond_32_bits():
     """a pool whose last page lies more than 2^32 bytes (and elements) behind its first"""
     d, hkv, page = 128, 8, 64
