@@ -39,7 +39,7 @@ constexpr int kFill = 4;                   // warps that convert or clean
 constexpr int kTile = 128;                 // rows of an M-tile, keys of a tile
 constexpr int kStep = 64;                  // keys of a step
 constexpr uint32_t kTmemCols = 512;
-constexpr float kNoRef = -1e30f;           // reference of a row that has seen no key: 2^(-inf - it) = 0
+constexpr float kNoRef = -3e38f;           // reference of a row that has seen no key: 2^(-inf - it) = 0, and any logit raises it
 // A row's reference is raised, and O rescaled, when a logit exceeds it by kSlack (log2), to kLow below the row's largest: most tiles
 // leave O alone, and fp16 weights go down to 2^-31 of the reference's.
 constexpr float kLow = 6.f, kSlack = 14.f;
@@ -101,7 +101,7 @@ __device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort));
 }
 
-// 2^x of two numbers x <= 2^20 on the FMA pipe, for a share of the weights: the special-function units take 8 cycles per warp and number, which
+// 2^x of two numbers x < 128 on the FMA pipe, for a share of the weights: the special-function units take 8 cycles per warp and number, which
 // bounds the softmax.  x = n + f, |f| <= 1/2, n by adding and subtracting 1.5 2^23; 2^f by a polynomial fitted here for least relative error
 // (2.6e-6; weights are rounded to 2^-9 or 2^-12); 2^n from its bits.  Below -127, and for -inf: 0.  NaN stays NaN.
 __device__ __forceinline__ void exp2_by_fma(float& x0, float& x1) {
@@ -121,15 +121,6 @@ __device__ __forceinline__ void exp2_by_fma(float& x0, float& x1) {
 }
 
 __device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7f80u) == 0x7f80u; }
-
-// The unit's place
-struct Unit {
-  CacheSeq s;
-  int seq, h, part, token0;
-  int pos0;                                // position of the sequence's first new token
-  int k0, k1;                              // keys of this part that some row sees
-  int first_lim;                           // last key that the unit's first row sees
-};
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -425,99 +416,99 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
     float m = kNoRef, l = 0.f;
     bool ok;
     do {
-    const float to_log2 = dm.scale * 1.44269504088896340736f * (kScaled && f16 ? __uint_as_float((uint32_t)(127 - sm.q_up[x * kTile + r] - kLift) << 23) : 1.f);
-    const uint64_t to_log2_2 = pack_f32x2(to_log2, to_log2);
-    m = kNoRef;
-    l = 0.f;
-    ok = true;
-    auto steps = [&](auto as_f16) {
-    constexpr bool kF16 = decltype(as_f16)::value;
-    // One weight in eight by the FMA pipe: chunk of 2048 495 -> 475 us, one in four 485, one in two 507.  Not where a quantised head_dim 128 leaves
-    // too few issue slots (569 -> 580).
-    constexpr bool kByFma = !kScaled || D == 64;
+      const float to_log2 = dm.scale * 1.44269504088896340736f * (kScaled && f16 ? __uint_as_float((uint32_t)(127 - sm.q_up[x * kTile + r] - kLift) << 23) : 1.f);
+      const uint64_t to_log2_2 = pack_f32x2(to_log2, to_log2);
+      m = kNoRef;
+      l = 0.f;
+      ok = true;
+      auto steps = [&](auto as_f16) {
+        constexpr bool kF16 = decltype(as_f16)::value;
+        // One weight in eight by the FMA pipe: chunk of 2048 495 -> 475 us, one in four 485, one in two 507.  Not where a quantised head_dim 128 leaves
+        // too few issue slots (569 -> 580).
+        constexpr bool kByFma = !kScaled || D == 64;
 #pragma unroll 1
-    for (int j = 0; j < n; ++j) {
-      ok = all_wait(&sm.s_full[x][j & 1], (j >> 1) & 1, abort);
-      if (!ok) break;
-      tc_fence_after_sync();
-      const uint32_t buf = s_addr + (j & 1) * kStep;
-      uint32_t v[2][32];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) tmem_ld32(buf + 32 * i, v[i]);
-      tmem_wait_ld();
-      const int base = k0 + j * kStep;
-      if (base + kStep - 1 > tile_lim) {
-        const int seen = lim - base;           // columns up to it are visible
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (32 * i + e > seen) v[i][e] = 0xff800000u;
-      }
-      // The weights are computed with the reference at hand, while the row's largest logit is looked for; where that is too large (in the
-      // first step, and seldom after it) they are computed again.
-      float sum;
-#pragma unroll 1
-      for (;;) {
-        const uint64_t neg_m = pack_f32x2(-m, -m);
-        uint64_t sum2[2];
-        float top[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t p[16];
-          sum2[i] = pack_f32x2(0.f, 0.f);
-          top[i] = __uint_as_float(v[i][0]);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float x0 = __uint_as_float(v[i][2 * e]), x1 = __uint_as_float(v[i][2 * e + 1]);
-            top[i] = fmaxf(top[i], fmaxf(x0, x1));
-            float a0, a1;
-            unpack_f32x2(fma_f32x2(pack_f32x2(x0, x1), to_log2_2, neg_m), a0, a1);
-            if (kByFma && (e & 7) == 5) {
-              exp2_by_fma(a0, a1);
-            } else {
-              a0 = fast_exp2(a0);
-              a1 = fast_exp2(a1);
-            }
-            sum2[i] = add_f32x2(sum2[i], pack_f32x2(a0, a1));
-            p[e] = kF16 ? pack_f16(a0, a1) : pack_bf16(a0, a1);
-          }
-          tmem_st16(buf + 16 * i, p);
-        }
-        float s0, s1;
-        unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
-        sum = s0 + s1;
-        const float mx = fmaxf(top[0], top[1]) * to_log2;
-        if (!__any_sync(0xffffffffu, mx > m + kSlack)) break;
-        const float now = fmaxf(m, mx - kLow), f = fast_exp2(m - now);
-        m = now;
-        l *= f;
-        if (j > 0) {
-          // O may be touched when P V of the step before is done
-          ok = all_wait(&sm.s_full[x][(j + 1) & 1], ((j + 1) >> 1) & 1, abort);
+        for (int j = 0; j < n; ++j) {
+          ok = all_wait(&sm.s_full[x][j & 1], (j >> 1) & 1, abort);
           if (!ok) break;
           tc_fence_after_sync();
-#pragma unroll 1
-          for (int c = 0; c < D; c += 16) {
-            uint32_t o[16];
-            tmem_ld16(o_addr + c, o);
-            tmem_wait_ld();
+          const uint32_t buf = s_addr + (j & 1) * kStep;
+          uint32_t v[2][32];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tmem_st16(o_addr + c, o);
+          for (int i = 0; i < 2; ++i) tmem_ld32(buf + 32 * i, v[i]);
+          tmem_wait_ld();
+          const int base = k0 + j * kStep;
+          if (base + kStep - 1 > tile_lim) {
+            const int seen = lim - base;           // columns up to it are visible
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (32 * i + e > seen) v[i][e] = 0xff800000u;
           }
+          // The weights are computed with the reference at hand, while the row's largest logit is looked for; where that is too large (in the
+          // first step, and seldom after it) they are computed again.
+          float sum;
+#pragma unroll 1
+          for (;;) {
+            const uint64_t neg_m = pack_f32x2(-m, -m);
+            uint64_t sum2[2];
+            float top[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              uint32_t p[16];
+              sum2[i] = pack_f32x2(0.f, 0.f);
+              top[i] = __uint_as_float(v[i][0]);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float x0 = __uint_as_float(v[i][2 * e]), x1 = __uint_as_float(v[i][2 * e + 1]);
+                top[i] = fmaxf(top[i], fmaxf(x0, x1));
+                float a0, a1;
+                unpack_f32x2(fma_f32x2(pack_f32x2(x0, x1), to_log2_2, neg_m), a0, a1);
+                if (kByFma && (e & 7) == 5) {
+                  exp2_by_fma(a0, a1);
+                } else {
+                  a0 = fast_exp2(a0);
+                  a1 = fast_exp2(a1);
+                }
+                sum2[i] = add_f32x2(sum2[i], pack_f32x2(a0, a1));
+                p[e] = kF16 ? pack_f16(a0, a1) : pack_bf16(a0, a1);
+              }
+              tmem_st16(buf + 16 * i, p);
+            }
+            float s0, s1;
+            unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
+            sum = s0 + s1;
+            const float mx = fmaxf(top[0], top[1]) * to_log2;
+            if (!__any_sync(0xffffffffu, mx > m + kSlack)) break;
+            const float now = fmaxf(m, mx - kLow), f = fast_exp2(m - now);
+            m = now;
+            l *= f;
+            if (j > 0) {
+              // O may be touched when P V of the step before is done
+              ok = all_wait(&sm.s_full[x][(j + 1) & 1], ((j + 1) >> 1) & 1, abort);
+              if (!ok) break;
+              tc_fence_after_sync();
+#pragma unroll 1
+              for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                tmem_ld16(o_addr + c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tmem_st16(o_addr + c, o);
+              }
+            }
+          }
+          if (!ok) break;
+          l += sum;
+          tmem_wait_st();
+          tc_fence_before_sync();
+          mbar_arrive_warp(&sm.p_full[x][j & 1]);
         }
-      }
-      if (!ok) break;
-      l += sum;
-      tmem_wait_st();
-      tc_fence_before_sync();
-      mbar_arrive_warp(&sm.p_full[x][j & 1]);
-    }
-    };
-    if (f16) steps(std::true_type{});
-    else steps(std::false_type{});
-    if (ok && n > 0) ok = all_wait(&sm.s_full[x][(n + 1) & 1], ((n + 1) >> 1) & 1, abort);      // P V of the last step
+      };
+      if (f16) steps(std::true_type{});
+      else steps(std::false_type{});
+      if (ok && n > 0) ok = all_wait(&sm.s_full[x][(n + 1) & 1], ((n + 1) >> 1) & 1, abort);      // P V of the last step
     } while (again());
     if (!*abort && n_tok > x * plan.tokens) {
       tc_fence_after_sync();
@@ -591,197 +582,197 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
     do {
-    if (warp < 10) {
-      // ---------------------------------------------------------------- GEMMs (the whole warp stays together, one lane issues)
-      const int x = warp - 8, n = x ? n1 : n0;
-      const uint32_t lead = elect_one();
-      constexpr uint32_t kBf16 = (1u << 7) | (1u << 10);      // formats of A and B: bf16, else fp16
-      const uint32_t type = f16 ? kBf16 : 0;
-      const uint32_t idesc_s = idesc_bf16_f32(128, kStep, 0, 0) ^ type, idesc_o = idesc_bf16_f32(128, D, 0, 1) ^ type;
-      const uint64_t q_desc = smem_desc_sw128(smem_u32(sm.q[x]), 16, 1024);
-      const uint64_t k_desc = smem_desc_sw128(smem_u32(sm.ring), 16, 1024), v_desc = smem_desc_sw128(smem_u32(sm.ring), kTile * 128, 1024);
-      const uint32_t s_tmem = tmem + x * kTile, o_tmem = tmem + 2 * kTile + x * D;
-      // a step is half a tile: 64 rows of 128 bytes per panel
-      auto issue_s = [&](int half, int slot) {
-        const uint64_t b = desc_advance(k_desc, slot * Sm::kTileBytes + half * (kStep * 128));
+      if (warp < 10) {
+        // ---------------------------------------------------------------- GEMMs (the whole warp stays together, one lane issues)
+        const int x = warp - 8, n = x ? n1 : n0;
+        const uint32_t lead = elect_one();
+        constexpr uint32_t kBf16 = (1u << 7) | (1u << 10);      // formats of A and B: bf16, else fp16
+        const uint32_t type = f16 ? kBf16 : 0;
+        const uint32_t idesc_s = idesc_bf16_f32(128, kStep, 0, 0) ^ type, idesc_o = idesc_bf16_f32(128, D, 0, 1) ^ type;
+        const uint64_t q_desc = smem_desc_sw128(smem_u32(sm.q[x]), 16, 1024);
+        const uint64_t k_desc = smem_desc_sw128(smem_u32(sm.ring), 16, 1024), v_desc = smem_desc_sw128(smem_u32(sm.ring), kTile * 128, 1024);
+        const uint32_t s_tmem = tmem + x * kTile, o_tmem = tmem + 2 * kTile + x * D;
+        // a step is half a tile: 64 rows of 128 bytes per panel
+        auto issue_s = [&](int half, int slot) {
+          const uint64_t b = desc_advance(k_desc, slot * Sm::kTileBytes + half * (kStep * 128));
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const uint32_t off = (i >> 2) * (kTile * 128) + (i & 3) * 32;
-          mma_ss_w(lead, s_tmem + half * kStep, desc_advance(q_desc, off), desc_advance(b, off), idesc_s, i > 0);
-        }
-      };
-      auto issue_pv = [&](int half, int slot, bool add) {
-        const uint64_t b = desc_advance(v_desc, slot * Sm::kTileBytes + half * (kStep * 128));
+          for (int i = 0; i < D / 16; ++i) {
+            const uint32_t off = (i >> 2) * (kTile * 128) + (i & 3) * 32;
+            mma_ss_w(lead, s_tmem + half * kStep, desc_advance(q_desc, off), desc_advance(b, off), idesc_s, i > 0);
+          }
+        };
+        auto issue_pv = [&](int half, int slot, bool add) {
+          const uint64_t b = desc_advance(v_desc, slot * Sm::kTileBytes + half * (kStep * 128));
 #pragma unroll
-        for (int i = 0; i < kStep / 16; ++i) mma_ts_w(lead, o_tmem, s_tmem + half * kStep + 8 * i, desc_advance(b, i * 2048), idesc_o, add || i > 0);
-      };
-      // Position in the ring of K(j) is 2j, of V(j) 2j + 1.  Both warps release every slot, whether its keys concern their M-tile or not,
-      // and always by a commit.
-      int slot = 0;
-      uint32_t phase = 0;
-      auto next = [&]() { if (++slot == NS) { slot = 0; phase ^= 1; } };
-      bool ok = true;
-      if (n_tiles > 0) {
-        ok = all_wait(&sm.full[0], 0, abort);
-        if (ok) {
-          tc_fence_after_sync();
+          for (int i = 0; i < kStep / 16; ++i) mma_ts_w(lead, o_tmem, s_tmem + half * kStep + 8 * i, desc_advance(b, i * 2048), idesc_o, add || i > 0);
+        };
+        // Position in the ring of K(j) is 2j, of V(j) 2j + 1.  Both warps release every slot, whether its keys concern their M-tile or not,
+        // and always by a commit.
+        int slot = 0;
+        uint32_t phase = 0;
+        auto next = [&]() { if (++slot == NS) { slot = 0; phase ^= 1; } };
+        bool ok = true;
+        if (n_tiles > 0) {
+          ok = all_wait(&sm.full[0], 0, abort);
+          if (ok) {
+            tc_fence_after_sync();
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            if (half < n) issue_s(half, 0);
+            for (int half = 0; half < 2; ++half) {
+              if (half < n) issue_s(half, 0);
+              mma_commit_w(lead, &sm.s_full[x][half]);
+            }
+            mma_commit_w(lead, &sm.empty[0]);
+            next();
+          }
+        }
+#pragma unroll 1
+        for (int j = 0; ok && j < n_tiles; ++j) {
+          const int v_slot = slot;
+          const bool more = j + 1 < n_tiles;
+          ok = all_wait(&sm.full[v_slot], phase, abort);
+          next();
+          const int k_slot = slot;
+          if (ok && more) ok = all_wait(&sm.full[k_slot], phase, abort);
+#pragma unroll 1
+          for (int half = 0; ok && half < 2; ++half) {
+            const int step = 2 * j + half;
+            if (step >= n) break;
+            ok = all_wait(&sm.p_full[x][half], j & 1, abort);
+            if (!ok) break;
+            tc_fence_after_sync();
+            issue_pv(half, v_slot, step > 0);
+            if (step + 2 < n) issue_s(half, k_slot);
             mma_commit_w(lead, &sm.s_full[x][half]);
           }
-          mma_commit_w(lead, &sm.empty[0]);
-          next();
-        }
-      }
-#pragma unroll 1
-      for (int j = 0; ok && j < n_tiles; ++j) {
-        const int v_slot = slot;
-        const bool more = j + 1 < n_tiles;
-        ok = all_wait(&sm.full[v_slot], phase, abort);
-        next();
-        const int k_slot = slot;
-        if (ok && more) ok = all_wait(&sm.full[k_slot], phase, abort);
-#pragma unroll 1
-        for (int half = 0; ok && half < 2; ++half) {
-          const int step = 2 * j + half;
-          if (step >= n) break;
-          ok = all_wait(&sm.p_full[x][half], j & 1, abort);
           if (!ok) break;
-          tc_fence_after_sync();
-          issue_pv(half, v_slot, step > 0);
-          if (step + 2 < n) issue_s(half, k_slot);
-          mma_commit_w(lead, &sm.s_full[x][half]);
+          mma_commit_w(lead, &sm.empty[v_slot]);
+          if (more) {
+            mma_commit_w(lead, &sm.empty[k_slot]);
+            next();
+          }
         }
-        if (!ok) break;
-        mma_commit_w(lead, &sm.empty[v_slot]);
-        if (more) {
-          mma_commit_w(lead, &sm.empty[k_slot]);
-          next();
+      } else {
+        // ---------------------------------------------------------------- copies (tile 0 went ahead)
+        for (int j = f16 == kScaled ? 1 : 0; j < n_tiles; ++j)
+          if (!copy_tile(j)) break;
+        if (bad_page) cache_status(status_word, HGA_STATUS_BAD_INDEX);
+        if (*abort && lane == 0) {
+          // giving up: give the copies still in flight time to land before shared memory is released
+          for (int it = 0; it < 64; ++it) __nanosleep(1000);
         }
       }
-    } else {
-      // ---------------------------------------------------------------- copies (tile 0 went ahead)
-      for (int j = f16 == kScaled ? 1 : 0; j < n_tiles; ++j)
-        if (!copy_tile(j)) break;
-      if (bad_page) cache_status(status_word, HGA_STATUS_BAD_INDEX);
-      if (*abort && lane == 0) {
-        // giving up: give the copies still in flight time to land before shared memory is released
-        for (int it = 0; it < 64; ++it) __nanosleep(1000);
-      }
-    }
     } while (again());
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRestRegs));
     const int w = warp - 12;
     do {
-    bool strange = false;
-    if (FMT == kCacheBf16) {
-      // ---------------------------------------------------------------- V tiles with hidden keys: a thread per key
-      const int r = tid & 127;
-      uint32_t parity = 0;                     // of each slot's raw_full
+      bool strange = false;
+      if (FMT == kCacheBf16) {
+        // ---------------------------------------------------------------- V tiles with hidden keys: a thread per key
+        const int r = tid & 127;
+        uint32_t parity = 0;                     // of each slot's raw_full
 #pragma unroll 1
-      for (int j = first_dirty; j < n_tiles; ++j) {
-        const int slot = (2 * j + 1) % NS;
-        if (!all_wait(&sm.raw_full[slot], (parity >> slot) & 1, abort)) break;
-        parity ^= 1u << slot;
-        const int key = k0 + j * kTile + r;
-        if (key > first_lim) {
+        for (int j = first_dirty; j < n_tiles; ++j) {
+          const int slot = (2 * j + 1) % NS;
+          if (!all_wait(&sm.raw_full[slot], (parity >> slot) & 1, abort)) break;
+          parity ^= 1u << slot;
+          const int key = k0 + j * kTile + r;
+          if (key > first_lim) {
 #pragma unroll 4
-          for (int c = 0; c < C; ++c) {
-            uint4* at16 = reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, c));
-            if (key >= k1) {
-              *at16 = make_uint4(0, 0, 0, 0);
-              continue;
-            }
-            uint4 y = *at16;
-            uint32_t* e = &y.x;
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (not_finite(e[i])) { e[i] &= 0xffff0000u; odd = true; }
-              if (not_finite(e[i] >> 16)) { e[i] &= 0xffffu; odd = true; }
-            }
-            if (odd) { *at16 = y; strange = true; }
-          }
-        }
-        fence_proxy_async_smem();
-        mbar_arrive_warp(&sm.full[slot]);
-      }
-    } else {
-      // ---------------------------------------------------------------- quantised tiles: converted from one buffer into another
-      constexpr int LPR = cache_row_bytes(FMT, D) / 16;        // lanes of a row
-      constexpr int RPI = 32 / LPR, kRows = kFill * RPI;       // rows of a warp's access, of all warps' (a multiple of 8)
-      constexpr int kPairs = FMT == kCacheMx8 ? 2 : 4;         // 16-byte pieces of bf16 or fp16 that a lane's 16 bytes become
-      const int in_row = lane % LPR, r0 = w * RPI + lane / LPR;
-      bool wide = false;
-      auto convert = [&](auto as_f16) {
-        constexpr bool kF16 = decltype(as_f16)::value;
-#pragma unroll 1
-        for (int i_ring = 0; i_ring < 2 * n_tiles; ++i_ring) {
-          const int use = i_ring / NS, slot = i_ring - use * NS, j = i_ring >> 1;
-          const bool is_v = i_ring & 1;
-          if (!all_wait(&sm.raw_full[i_ring & 1], (i_ring >> 1) & 1, abort) || !all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
-          const uint8_t* src = sm.raw[i_ring & 1] + r0 * cache_row_bytes(FMT, D) + in_row * 16;
-          const uint8_t* scales = sm.raw[i_ring & 1] + Sm::kRaw + r0 * (D / 32) + (FMT == kCacheMx8 ? in_row >> 1 : in_row);
-          uint8_t* dst = sm.ring[slot];
-          const int end = k1 - (k0 + j * kTile) - r0, hidden = is_v ? first_lim - (k0 + j * kTile) - r0 : kTile;      // rows from `end` on are none
-#pragma unroll
-          for (int i = 0; i < kTile / kRows; ++i) {
-            uint4 y = *reinterpret_cast<const uint4*>(src + i * kRows * cache_row_bytes(FMT, D));
-            uint32_t sc = scales[i * kRows * (D / 32)];
-            if (i * kRows >= end) {
-              y = make_uint4(0, 0, 0, 0);
-              sc = 127;
-            }
-            const uint32_t q[4] = {y.x, y.y, y.z, y.w};
-            uint32_t o[4 * kPairs], mul;
-            if (kF16) {
-              const uint32_t e = sc - (127 - kLift - 15);
-              mul = e * 0x04000400u;
-              if (e - 1 >= kTop + 15) {          // out of range: zeros (2^-127 counts as zero), NaN, or a number that is too large or small
-                if (sc == 255 && i * kRows > hidden) { sc = 0; strange = true; }
-                mul = sc == 255 ? 0x7e007e00u : 0u;
-                wide = wide || (sc != 0 && sc != 255);
+            for (int c = 0; c < C; ++c) {
+              uint4* at16 = reinterpret_cast<uint4*>(sm.ring[slot] + piece<D>(r, c));
+              if (key >= k1) {
+                *at16 = make_uint4(0, 0, 0, 0);
+                continue;
               }
+              uint4 y = *at16;
+              uint32_t* e = &y.x;
+              bool odd = false;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                if (FMT == kCacheMx8) e4m3x4_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1]);
-                else e2m1x8_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1], o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
-#pragma unroll
-                for (int z = 0; z < kPairs; ++z) o[k * kPairs + z] = mul_f16x2(o[k * kPairs + z], mul);
+              for (int i = 0; i < 4; ++i) {
+                if (not_finite(e[i])) { e[i] &= 0xffff0000u; odd = true; }
+                if (not_finite(e[i] >> 16)) { e[i] &= 0xffffu; odd = true; }
               }
-            } else {
-              if (sc == 255 && i * kRows > hidden) { sc = 0; strange = true; }
-              mul = pair(scale_bits(sc));
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                if (FMT == kCacheMx8) {
-                  o[k * kPairs] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x1404)), kTwo120), mul);
-                  o[k * kPairs + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x3424)), kTwo120), mul);
-                } else {
-                  e2m1x4_to_bf16(q[k] & 0xffffu, o[k * kPairs], o[k * kPairs + 1]);
-                  e2m1x4_to_bf16(q[k] >> 16, o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
-#pragma unroll
-                  for (int z = 0; z < kPairs; ++z) o[k * kPairs + z] = mul_bf16x2(o[k * kPairs + z], mul);
-                }
-              }
+              if (odd) { *at16 = y; strange = true; }
             }
-            // (Storing the pieces so that no two lanes meet a bank takes selections that cost more than the conflicts: 581 against 567 us.)
-#pragma unroll
-            for (int k = 0; k < kPairs; ++k)
-              *reinterpret_cast<uint4*>(dst + piece<D>(r0, kPairs * in_row + k) + i * kRows * 128) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
           }
           fence_proxy_async_smem();
           mbar_arrive_warp(&sm.full[slot]);
-          mbar_arrive_warp(&sm.raw_empty[i_ring & 1]);
         }
-      };
-      if (f16) convert(std::true_type{});
-      else convert(std::false_type{});
-      if (wide) sm.wide = 1;
-    }
-    if (strange) sm.strange = 1;
+      } else {
+        // ---------------------------------------------------------------- quantised tiles: converted from one buffer into another
+        constexpr int LPR = cache_row_bytes(FMT, D) / 16;        // lanes of a row
+        constexpr int RPI = 32 / LPR, kRows = kFill * RPI;       // rows of a warp's access, of all warps' (a multiple of 8)
+        constexpr int kPairs = FMT == kCacheMx8 ? 2 : 4;         // 16-byte pieces of bf16 or fp16 that a lane's 16 bytes become
+        const int in_row = lane % LPR, r0 = w * RPI + lane / LPR;
+        bool wide = false;
+        auto convert = [&](auto as_f16) {
+          constexpr bool kF16 = decltype(as_f16)::value;
+#pragma unroll 1
+          for (int i_ring = 0; i_ring < 2 * n_tiles; ++i_ring) {
+            const int use = i_ring / NS, slot = i_ring - use * NS, j = i_ring >> 1;
+            const bool is_v = i_ring & 1;
+            if (!all_wait(&sm.raw_full[i_ring & 1], (i_ring >> 1) & 1, abort) || !all_wait(&sm.empty[slot], (use & 1) ^ 1, abort)) break;
+            const uint8_t* src = sm.raw[i_ring & 1] + r0 * cache_row_bytes(FMT, D) + in_row * 16;
+            const uint8_t* scales = sm.raw[i_ring & 1] + Sm::kRaw + r0 * (D / 32) + (FMT == kCacheMx8 ? in_row >> 1 : in_row);
+            uint8_t* dst = sm.ring[slot];
+            const int end = k1 - (k0 + j * kTile) - r0, hidden = is_v ? first_lim - (k0 + j * kTile) - r0 : kTile;      // rows from `end` on are none
+#pragma unroll
+            for (int i = 0; i < kTile / kRows; ++i) {
+              uint4 y = *reinterpret_cast<const uint4*>(src + i * kRows * cache_row_bytes(FMT, D));
+              uint32_t sc = scales[i * kRows * (D / 32)];
+              if (i * kRows >= end) {
+                y = make_uint4(0, 0, 0, 0);
+                sc = 127;
+              }
+              const uint32_t q[4] = {y.x, y.y, y.z, y.w};
+              uint32_t o[4 * kPairs], mul;
+              if (kF16) {
+                const uint32_t e = sc - (127 - kLift - 15);
+                mul = e * 0x04000400u;
+                if (e - 1 >= kTop + 15) {          // out of range: zeros (2^-127 counts as zero), NaN, or a number that is too large or small
+                  if (sc == 255 && i * kRows > hidden) { sc = 0; strange = true; }
+                  mul = sc == 255 ? 0x7e007e00u : 0u;
+                  wide = wide || (sc != 0 && sc != 255);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  if (FMT == kCacheMx8) e4m3x4_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1]);
+                  else e2m1x8_to_f16(q[k], o[k * kPairs], o[k * kPairs + 1], o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
+#pragma unroll
+                  for (int z = 0; z < kPairs; ++z) o[k * kPairs + z] = mul_f16x2(o[k * kPairs + z], mul);
+                }
+              } else {
+                if (sc == 255 && i * kRows > hidden) { sc = 0; strange = true; }
+                mul = pair(scale_bits(sc));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  if (FMT == kCacheMx8) {
+                    o[k * kPairs] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x1404)), kTwo120), mul);
+                    o[k * kPairs + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x3424)), kTwo120), mul);
+                  } else {
+                    e2m1x4_to_bf16(q[k] & 0xffffu, o[k * kPairs], o[k * kPairs + 1]);
+                    e2m1x4_to_bf16(q[k] >> 16, o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);
+#pragma unroll
+                    for (int z = 0; z < kPairs; ++z) o[k * kPairs + z] = mul_bf16x2(o[k * kPairs + z], mul);
+                  }
+                }
+              }
+              // (Storing the pieces so that no two lanes meet a bank takes selections that cost more than the conflicts: 581 against 567 us.)
+#pragma unroll
+              for (int k = 0; k < kPairs; ++k)
+                *reinterpret_cast<uint4*>(dst + piece<D>(r0, kPairs * in_row + k) + i * kRows * 128) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            }
+            fence_proxy_async_smem();
+            mbar_arrive_warp(&sm.full[slot]);
+            mbar_arrive_warp(&sm.raw_empty[i_ring & 1]);
+          }
+        };
+        if (f16) convert(std::true_type{});
+        else convert(std::false_type{});
+        if (wide) sm.wide = 1;
+      }
+      if (strange) sm.strange = 1;
     } while (again());
   }
 
@@ -877,6 +868,12 @@ int launch_of(const CacheDims& dm, const Plan& plan, const void* Q, const int32_
   static_assert(sizeof(Smem<FMT, D>) + 1024 <= 232448, "shared memory of a CTA");
   const int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem, true);
   if (rc) return rc;
+  // the registers that the warps pass on to one another are those of the launch
+  static const int regs = [] {
+    cudaFuncAttributes a;
+    return cudaFuncGetAttributes(&a, reinterpret_cast<const void*>(k_cache_attn_sm100<FMT, D>)) == cudaSuccess ? a.numRegs : 0;
+  }();
+  if (regs < (2 * kSoftmaxRegs + kIssueRegs + kRestRegs) / 4) return HGA_ERR_UNSUPPORTED;
   PdlLaunch cfg(dim3((unsigned)ctas), kThreads, smem, st, 0);
   const cudaError_t e = cudaLaunchKernelEx(&cfg.c, kernel, mk, mv, dm, plan, (const uint16_t*)Q, cu_q, seq_lens, table, (const uint8_t*)K,
                                            (const uint8_t*)V, (const uint8_t*)K_scale, (const uint8_t*)V_scale, (uint16_t*)O, LSE,

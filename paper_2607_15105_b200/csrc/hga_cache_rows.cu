@@ -34,7 +34,7 @@ using namespace sm100;
 namespace {
 
 constexpr int kWarps = 4;
-constexpr float kNoRef = -1e30f;      // reference of a row without a key: 2^(-inf - it) = 0
+constexpr float kNoRef = -3e38f;      // reference of a row without a key: 2^(-inf - it) = 0, and any logit raises it
 constexpr float kLow = 6.f, kSlack = 14.f;      // log2: how far the reference is set below the largest logit, and may be exceeded
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {

@@ -422,6 +422,23 @@ def test_two_streams_with_workspaces_of_their_own():
         pr.check_attn(q, O, LSE)
 
 
+@pytest.mark.parametrize("new,length", ((1, 90), (1, 700), (1, 9000), (70, 200), (70, 3000)))
+@pytest.mark.parametrize("sign", (-1, 1))
+def test_large_logits_all_alike(new, length, sign):
+    """all logits at +-2^25: the mean of the values, whatever the way (one CTA, a cluster, parts, tiles)"""
+    pr = T.Problem([(new, length)], "bf16", hq=2, hkv=1, d=64, page=64, seed=25)
+    pr.K.fill_(2.0 ** 12)
+    Q = torch.full((pr.n_tokens, 2, 64), sign * 2.0 ** 10, dtype=torch.bfloat16, device="cuda")
+    O, LSE = pr.run_attn(Q)
+    V = pr.resident(pr.values("V"), 0)[0]
+    for j in (0, new - 1):
+        v = V[:length - new + j + 1]
+        # equal weights, each rounded alike; sums of up to 9000 values below 5 in fp32, the tensor pipe cutting off; O's rounding
+        off = 2.0 ** -8 * np.abs(v.mean(0)) + len(v) * 2.0 ** -23 * np.abs(v).mean(0)
+        assert (np.abs(T.f64(O[j, 0]) - v.mean(0)) <= off).all()
+        assert abs(LSE[j, 0].item() / (sign * 2.0 ** 25) - 1) < 1e-5
+
+
 def test_a_pool_that_is_not_on_the_current_device_is_refused():
     pr = T.Problem([(1, 9)], "bf16", hq=1, hkv=1, d=64, seed=23, device="cpu")
     with pytest.raises(ValueError, match="current device"):
