@@ -336,7 +336,7 @@ typedef struct hga_cache_params {
   int32_t n_tokens;                               /* rows of the packed tensors (all new tokens together)        */
   int32_t max_new;                                /* no sequence has more new tokens than this (>= 1)            */
   int32_t max_len;                                /* no seq_lens entry is larger than this; 0 = max_pages * page_size.  The
-                                                     closer, the better the work is shared out                    */
+                                                     closer, the better the work is shared out.  The smaller of the two: 2^30 at most */
   float   softmax_scale;                          /* <= 0 selects 1/sqrt(head_dim)                               */
   int32_t flags;                                  /* 0                                                           */
   int32_t reserved;                               /* 0                                                           */
@@ -368,7 +368,8 @@ HGA_API int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t
  * A row that sees no key gets O = 0 and LSE = -inf.  Rows outside cu_q are left as they were.  Keys and values that a row does not
  * see have no influence on it, not even infinities or NaN.  Products are of bf16 numbers (the cache's are), sums in fp32; the
  * probabilities are rounded to bf16 (over a quantised pool to fp16: off by 2^-11 of themselves, or 2^-31 of the row's largest).  Numbers of a
- * quantised pool below 2^-118 count as zeros.  Results do not depend on what else is in the batch, nor change from
+ * quantised pool below 2^-118 count as zeros, and of a query row those that are below 2^-29 of its largest or 2^-125 lose bits.  O overlaps no
+ * input.  Results do not depend on what else is in the batch, nor change from
  * run to run, except that max_len, max_new and n_seq decide how the keys are shared out.
  * workspace: device scratch of at least hga_cache_workspace_bytes() bytes (16-byte aligned; may be NULL where that is 0); contents
  * are overwritten.  Calls that share a workspace must not overlap. */

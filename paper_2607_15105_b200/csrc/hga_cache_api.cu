@@ -40,6 +40,7 @@ static int resolve_cache(const hga_cache_params* p, CacheDims& dm) {
   dm.max_new = std::min(p->max_new, std::max(p->n_tokens, 1));
   dm.max_keys = p->max_pages * p->page_size;
   if (p->max_len > 0) dm.max_keys = std::min(dm.max_keys, p->max_len);
+  if (dm.max_keys > 1 << 30) return HGA_ERR_SHAPE;      // (a position and the keys of a part behind it are an int)
   dm.scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)dm.d);
   if (p->table_stride != 0 && p->table_stride < p->max_pages) return HGA_ERR_SHAPE;
   dm.table_stride = p->table_stride ? p->table_stride : p->max_pages;
@@ -114,7 +115,7 @@ int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t tok_end
   if (misaligned(K_out) || misaligned(V_out) || misaligned(K_cache) || misaligned(V_cache) || misaligned(K_scale) || misaligned(V_scale) ||
       misaligned(seq_lens, 4) || misaligned(block_table, 4))
     return HGA_ERR_ALIGN;
-  if (tok_begin < 0 || tok_end < tok_begin) return HGA_ERR_SHAPE;
+  if (tok_begin < 0 || tok_end < tok_begin || tok_end > 0x7fffff00) return HGA_ERR_SHAPE;      // (rows of the last CTA are counted in an int)
   const int64_t n = tok_end - tok_begin, d = dm.d, dense[3] = {dm.Hkv * n * d, n * d, d};
   if ((rc = take_strides(p->out_stride, dm.outs, dense, 8, dm.d))) return rc;
   if (n > 0 && dm.outs[2] == 0) return HGA_ERR_SHAPE;

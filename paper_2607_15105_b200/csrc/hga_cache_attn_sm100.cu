@@ -20,6 +20,7 @@
 // unit's first row (the last ones), numbers that are not finite are replaced by zeros, rows behind the last key altogether, and the
 // rows that do see such numbers get them added at the end.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "hga_cache.cuh"
@@ -195,6 +196,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       for (int v = 0; v < units; ++v) ahead += steps[v] > mine || (steps[v] == mine && v < tid);
       if (ahead == rank) { sm.seq = seq; sm.token0 = t0; }
     }
+    fence_proxy_async_smem();                                  // (tiles will be copied over the table)
   } else if (warp == 0) {
     const int u = plan.units - 1 - rank;
     int seen = 0, seq = -1, t0 = 0;
@@ -818,7 +820,7 @@ Plan plan_of(const CacheDims& dm) {
   int k = 1;
   if (n < sms) {
     // few units: their keys are shared out, so that the device is full, the more the less even their lengths may be
-    k = dm.n_seq == 1 ? best_parts(n) : (2 * sms + n - 1) / n;
+    k = dm.n_seq == 1 || n == 0 ? best_parts(n) : (2 * sms + n - 1) / n;      // (n = 0: without tokens)
     if (dm.max_keys / k < 512) k = std::max(dm.max_keys / 512, 1);
   } else if (dm.n_seq == 1 && n % sms) {
     // the last round's, where that takes a tenth off: 1408 tokens behind 15K, 176 units: 467 us whole, 328 so (256 units, whose last round
@@ -869,10 +871,13 @@ int launch_of(const CacheDims& dm, const Plan& plan, const void* Q, const int32_
   const int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem, true);
   if (rc) return rc;
   // the registers that the warps pass on to one another are those of the launch
-  static const int regs = [] {
+  static std::atomic<int> regs{0};
+  if (regs == 0) {
     cudaFuncAttributes a;
-    return cudaFuncGetAttributes(&a, reinterpret_cast<const void*>(k_cache_attn_sm100<FMT, D>)) == cudaSuccess ? a.numRegs : 0;
-  }();
+    const cudaError_t e = cudaFuncGetAttributes(&a, reinterpret_cast<const void*>(kernel));
+    if (e != cudaSuccess) return record_cuda(e);
+    regs = a.numRegs;
+  }
   if (regs < (2 * kSoftmaxRegs + kIssueRegs + kRestRegs) / 4) return HGA_ERR_UNSUPPORTED;
   PdlLaunch cfg(dim3((unsigned)ctas), kThreads, smem, st, 0);
   const cudaError_t e = cudaLaunchKernelEx(&cfg.c, kernel, mk, mv, dm, plan, (const uint16_t*)Q, cu_q, seq_lens, table, (const uint8_t*)K,

@@ -194,7 +194,7 @@ k_cache_read(const CacheDims dm, int tok_begin, int n, const int32_t* seq_lens, 
   pdl_launch_dependents();
   const int len = seq_lens[i];
   bool bad = len < 0 || len > dm.max_keys;
-  const int end = min(min(len, dm.max_keys) - tok_begin, n);      // rows of this sequence that are there
+  const int end = min(min(max(len, 0), dm.max_keys) - tok_begin, n);      // rows of this sequence that are there
   const uint8_t* const k0 = K + h * dm.ks[1] * kUnit + c * sizeof(Raw);
   const uint8_t* const v0 = V + h * dm.vs[1] * kUnit + c * sizeof(Raw);
   Raw k[kReadRows][2], v[kReadRows][2];

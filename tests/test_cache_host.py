@@ -115,6 +115,27 @@ def test_nothing_to_do_is_no_error(lib, ptr):
     assert lib.hga_cache_read(C.byref(p), 5, 5, *[ptr] * 8, None, None) == 0
 
 
+@pytest.mark.parametrize("fmt", (binding.HGA_CACHE_BF16, binding.HGA_CACHE_MXFP8, binding.HGA_CACHE_MXFP4))
+@pytest.mark.parametrize("n_seq", (1, 2, 700))
+@pytest.mark.parametrize("hq", (2, 130, 256))
+def test_no_tokens_of_any_number_of_heads(lib, ptr, fmt, n_seq, hq):
+    p = params(n_seq=n_seq, n_q_heads=hq, n_tokens=0, max_pages=4096, max_len=0, fmt=fmt)
+    n = binding.hga_cache_workspace_bytes(p)
+    assert n == 0
+    assert lib.hga_cache_attn(C.byref(p), *[ptr] * 10, None, n, None, None) == 0
+
+
+def test_positions_that_an_int_does_not_hold(lib, ptr):
+    n = C.c_size_t()
+    far = params(max_pages=(1 << 26) + 1, max_len=0)           # pages of 16
+    assert lib.hga_cache_workspace_bytes(C.byref(far), C.byref(n)) == -2
+    assert calls(lib, far, ptr) == (-2,) * 3
+    assert binding.hga_cache_workspace_bytes(params(max_pages=(1 << 26) + 1, max_len=64)) == 0
+    one = params(n_seq=1, n_q_heads=1, n_kv_heads=1)
+    for end in (0x7fffffff, 0x7fffff01):
+        assert lib.hga_cache_read(C.byref(one), 0, end, *[ptr] * 8, None, None) == -2
+
+
 def test_formats_against_torch():
     codes = torch.arange(256, dtype=torch.uint8)
     want = codes.view(torch.float8_e4m3fn).double().numpy()

@@ -329,6 +329,15 @@ def test_broken_prefix_sums_stay_inside(cu, op):
     assert int(pr.status.item()) == binding.HGA_STATUS_BAD_INDEX
 
 
+def test_lengths_below_zero_are_read_as_none():
+    pr = T.Problem([(4, 30), (4, 40)], "mx8", hq=2, hkv=2, d=64, seed=31)
+    pr.d_lens = torch.tensor([-0x80000000, 40], dtype=torch.int32, device="cuda")
+    out = torch.full((2, 2, 25, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    binding.hga_cache_read(pr.p, 10, 35, pr.d_lens, pr.d_table, *pr.cache(), out, None, pr.status)
+    assert (out[0] == 9).all() and np.array_equal(T.f64(out[1]), pr.resident(pr.values("K"), 1)[:, 10:35])
+    assert int(pr.status.item()) == binding.HGA_STATUS_BAD_INDEX
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("seqs", ([(1, 300)], [(90, 300)]))
 def test_large_logits_in_any_order(fmt, seqs):
