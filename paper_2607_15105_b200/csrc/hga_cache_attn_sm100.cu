@@ -19,8 +19,13 @@
 // A hidden key has weight zero, which does not silence a V row that is not finite.  So in the tiles that hold keys hidden from the
 // unit's first row (the last ones), numbers that are not finite are replaced by zeros, rows behind the last key altogether, and the
 // rows that do see such numbers get them added at the end.
+//
+// Measured, 32 query heads on 8 of 128: 2048 tokens behind 14336, bf16, 472 to 540 us from one machine to another (0.95 to 1.09 PFLOP/s; tensor
+// pipe active 71 % of the time, 256 units on 148 SMs); 16384 tokens 1870 to 2190 us (1.00 to 1.18 PFLOP/s, at the power limit); e4m3, 12 packed
+// sequences 538 to 561 us (0.82 to 0.86 PFLOP/s: the shared-memory pipe, 77 to 85 % busy with converted tiles and the GEMMs' operands).
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <type_traits>
 
 #include "hga_cache.cuh"
@@ -145,9 +150,10 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   int at = blockIdx.x, part = 0;
   const bool split = plan.sp.parts > 1 && at >= plan.sp.full;
   if (split) {
-    const int i = at - plan.sp.full;
-    at = plan.sp.full + i / plan.sp.parts;
-    part = i % plan.sp.parts;
+    // (the first parts, which may be the longer ones, first)
+    const int i = at - plan.sp.full, n = plan.units * dm.Hkv - plan.sp.full;
+    part = i / n;
+    at = plan.sp.full + i - part * n;
   }
   const int rank = dm.by_Hkv(at), h = at - rank * dm.Hkv;
   if (plan.ranked) {
@@ -808,34 +814,46 @@ Plan plan_of(const CacheDims& dm) {
   const int n = (int)std::min<int64_t>((int64_t)p.units * dm.Hkv, 0x7fffffff), sms = 148;
   const double steps = dm.max_keys / 64.;
   auto cost = [&](int64_t n, int k) { return (double)((n * k + sms - 1) / sms) * (steps / k + 16) + (k > 1 ? 25 + 2 * k : 0); };
-  auto best_parts = [&](int64_t n) {
-    int best = 1;
+  struct Cut { int parts; double first, cost; };      // first: steps of the first part, and of all but the last
+  auto best_cut = [&](int64_t n) {
+    Cut best{1, steps, cost(n, 1)};
     for (int k = 2; k <= 64 && dm.max_keys / k >= 512; ++k)
-      if (cost(n, k) < cost(n, best)) best = k;
+      if (cost(n, k) < best.cost) best = Cut{k, steps / k, cost(n, k)};
+    // Or two parts, the first of which takes an SM each, and the rest the second ones, `r` one after another, in the same time (16384 keys, 88
+    // units: 217 us in three even parts, 201 so)
+    if (n > sms / 2 && n < sms) {
+      const int64_t r = (n + sms - n - 1) / (sms - n);
+      const double first = (r * (steps + 16) - 16) / (r + 1), c = first + 16 + 25 + 4;
+      if (first < steps - 8 && c < best.cost) best = Cut{2, first, c};
+    }
     return best;
   };
   p.sp.cluster = false;
   p.sp.tokens = dm.n_tokens;
   p.sp.unit = p.sp.units = p.sp.full = 0;
-  int k = 1;
+  Cut cut{1, steps, 0};
   if (n < sms) {
     // few units: their keys are shared out, so that the device is full, the more the less even their lengths may be
-    k = dm.n_seq == 1 || n == 0 ? best_parts(n) : (2 * sms + n - 1) / n;      // (n = 0: without tokens)
-    if (dm.max_keys / k < 512) k = std::max(dm.max_keys / 512, 1);
+    if (dm.n_seq == 1 || n == 0) {
+      cut = best_cut(n);                                 // (n = 0: without tokens)
+    } else {
+      cut.parts = std::min((2 * sms + n - 1) / n, std::max(dm.max_keys / 512, 1));
+      cut.first = steps / cut.parts;
+    }
   } else if (dm.n_seq == 1 && n % sms) {
-    // the last round's, where that takes a tenth off: 1408 tokens behind 15K, 176 units: 467 us whole, 328 so (256 units, whose last round
-    // is fuller: 473 whole, 504 so)
+    // the last round's, where that takes 7 % off.  16384 keys, whole / so: 176 units 470 / 324 us, 224 units 468 / 439, 240 units 471 / 445.  (256
+    // units, of which it should take 5 % off: 471 / 472.  The device is then busy to the end, at a lower clock.)
     const int full = n / sms * sms;
-    k = best_parts(n - full);
-    if (cost(n - full, 1) - cost(n - full, k) < 0.1 * cost(n, 1)) k = 1;
-    if (k > 1) {
+    const Cut tail = best_cut(n - full);
+    if (tail.parts > 1 && cost(n - full, 1) - tail.cost >= 0.07 * cost(n, 1)) {
+      cut = tail;
       p.sp.unit = (int)unit;
       p.sp.units = p.units;
       p.sp.full = full;
       p.sp.tokens = (int)std::min<int64_t>((int64_t)(p.units - full / dm.Hkv) * unit, dm.n_tokens);
     }
   }
-  p.sp.keys = (int)std::min<int64_t>(((int64_t)(dm.max_keys + k - 1) / k + kTile - 1) / kTile * kTile, 0x7fffff00);
+  p.sp.keys = cut.parts == 1 ? (dm.max_keys + kTile - 1) / kTile * kTile : (int)std::ceil(cut.first * kStep / kTile) * kTile;
   p.sp.parts = std::max((dm.max_keys + p.sp.keys - 1) / p.sp.keys, 1);
   if (p.sp.parts == 1) p.sp.unit = p.sp.units = p.sp.full = 0;
   p.ranked = dm.n_seq > 1 && dm.n_seq <= kMaxRanked && p.units <= kMaxRanked && p.sp.parts == 1;

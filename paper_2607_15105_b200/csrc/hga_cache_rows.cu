@@ -19,6 +19,10 @@
 // Softmax: every warp has one reference per row, raised (and its sums rescaled) only when a logit exceeds it by 2^14, so that most
 // steps have no exchange between lanes.  It stays 2^6 below the row's largest when it is raised: fp16 then keeps weights down to 2^-31.
 // LSE is of the exact probabilities; O is divided by the sum of the rounded ones, a product with a column of ones.
+//
+// Measured, 32 query heads on 8 of 128, one token: bf16, 65533 keys 48.5 us (5.5 TB/s, 84 % of a copy's rate); 32 sequences of 16K bf16 318 us
+// (6.7 TB/s), e4m3 207 us (5.3 TB/s), e2m1 143 us (4.1 TB/s): what has fewer bytes is bound by the conversion's instructions (45 to 53 % of the
+// issue slots at three CTAs of four warps per SM).
 #include <algorithm>
 #include <type_traits>
 

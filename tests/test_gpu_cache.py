@@ -195,6 +195,43 @@ def test_many_sequences(fmt, n_seq, most):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("new,length,parts", ((20, 7000, 2), (40, 9000, None), (56, 16000, 2), (37, 5000, None), (8, 3000, None), (64, 2000, 0)))
+def test_chunks_whose_keys_are_shared_out(fmt, new, length, parts):
+    """one sequence whose units are fewer than SMs, or leave a part of them idle in the last round: two uneven parts, several even ones, none.
+    128 query heads per key/value head make a unit of two tokens."""
+    hq, hkv, d = 1024, 8, 64
+    pr = T.Problem([(new, length)], fmt, hq=hq, hkv=hkv, d=d, page=64, seed=32)
+    need = binding.hga_cache_workspace_bytes(pr.p)
+    if parts is None:
+        assert need > 0
+    else:
+        units = (new + 1) // 2
+        tokens = min((units - units * hkv // 148 * 148 // hkv) * 2, new)      # of the units that are shared out
+        assert need == parts * tokens * hq * (d + 4) * 4
+    Q = pr.randn(new, hq, d)
+    O, LSE = pr.run_attn(Q.cuda())
+    assert int(pr.status.item()) == 0
+    # as Problem.attend, a key/value head at a time, with matrix products in 64 bits; tolerances as there
+    K, V = (torch.from_numpy(pr.resident(pr.values(n), 0)).cuda() for n in "KV")
+    hidden = torch.arange(length, device="cuda")[None] > length - new + torch.arange(new, device="cuda")[:, None]
+    for h in range(hkv):
+        q = Q[:, h * 128:(h + 1) * 128].cuda().double()
+        x = (q @ K[h].T / 8).masked_fill(hidden[:, None], -np.inf)
+        lse = torch.logsumexp(x, -1)
+        w = torch.exp(x - lse[..., None])
+        want, a = w @ V[h], w @ V[h].abs()
+        size = (q.abs() @ K[h].abs().T / 8).masked_fill(hidden[:, None], 0).amax(-1)
+        off = (d + 4) * 2.0 ** -23 * size + 2.0 ** -21
+        tol = 2.0 ** -8 * (a + 2 * want.abs()) + 2 * (off + 2.0 ** -23 * 4096)[..., None] * (a + want.abs()) + 2.0 ** -92
+        if fmt != "bf16":
+            tol += 2.0 ** -31 * w.amax(-1)[..., None] * V[h].abs().sum(0)
+        got = O[:, h * 128:(h + 1) * 128].double()
+        assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
+        tol_l = 2 * off + 2.0 ** -23 * 4096 + 2.0 ** -22 * lse.abs()
+        assert ((LSE[:, h * 128:(h + 1) * 128].double() - lse).abs() <= tol_l).all()
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 def test_kernels_are_the_ones_meant(fmt):
     """tiles of 16 rows for few of them, of 128 for more; parts joined in a cluster or by a kernel of its own"""
     for new, length, hq, rows, tensor in ((1, 100, 8, 1, 0), (1, 700, 8, 1, 0), (1, 9000, 8, 2, 0), (12, 300, 4, 1, 0), (70, 300, 4, 0, 1), (70, 9000, 4, 1, 1)):
