@@ -306,13 +306,14 @@ HGA_API int hga_varlen_workspace_bytes(const hga_params* p, int32_t n_seq, const
  * The pool is K_cache and V_cache [n_pages, Hkv, page_size, row] (any order of the first three axes, by strides).  Sequence i's
  * token at position t lies in row t % page_size of page block_table[i, t / page_size].  A row holds head_dim numbers:
  *   HGA_CACHE_BF16   head_dim bf16
- *   HGA_CACHE_MXFP8  head_dim bytes e4m3, and head_dim/32 scale bytes
+ *   HGA_CACHE_MXFP8  head_dim bytes e4m3 (0x7f and 0xff are NaN), and head_dim/32 scale bytes
  *   HGA_CACHE_MXFP4  head_dim/2 bytes, two e2m1 each (the even element in the low half), and head_dim/32 scale bytes
  * Scale byte s of a block of 32 consecutive elements stands for 2^(s - 127); a number is (element value) * 2^(s - 127).  hga_cache_write
  * takes the smallest power, s >= 0, that brings the block's largest magnitude to the element type's largest value (448, 6) or
  * below, and rounds each element once, to nearest, ties to even; so nothing saturates, and every number held is exactly a bf16 number.
  * (Elements that would round to 2^128, past bf16's range, are rounded toward zero.)  A block with an infinity or a NaN gets s = 255
- * and reads back as NaN.  K_scale, V_scale: uint8 [n_pages, Hkv, page_size, head_dim/32], dense; not used with HGA_CACHE_BF16.
+ * and reads back as NaN.  (In a pool that another program filled: e4m3's NaN codes, which hga_cache_write does not make, are NaN under
+ * any scale.)  K_scale, V_scale: uint8 [n_pages, Hkv, page_size, head_dim/32], dense; not used with HGA_CACHE_BF16.
  *
  * The calls of one step take the same description of it, in DEVICE memory, so that a captured step can be replayed with other
  * contents:

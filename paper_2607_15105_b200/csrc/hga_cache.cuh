@@ -98,6 +98,14 @@ __device__ __forceinline__ void e2m1x4_to_bf16(uint32_t w, uint32_t& r0, uint32_
   r1 = __byte_perm(lo, hi, 0x7362) | ((w << 4) & 0x8000u) | ((w << 16) & 0x80000000u);
 }
 
+// The bytes of a word that are e4m3's NaN (0x7f, 0xff), by their top bits; and bytes 0 and 1, or 2 and 3, of these as halves of 0x7fff, which
+// make a NaN of any bf16 number
+__device__ __forceinline__ uint32_t e4m3_nan(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t nan_halves(uint32_t top_bits, bool upper) {
+  const uint32_t h = __byte_perm(top_bits, 0, upper ? 0x3424 : 0x1404);
+  return h - (h >> 15);
+}
+
 // Four e4m3 / eight e2m1 numbers of a word as fp16 pairs, the lowest first
 __device__ __forceinline__ void e4m3x4_to_f16(uint32_t x, uint32_t& r0, uint32_t& r1) {
   asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"

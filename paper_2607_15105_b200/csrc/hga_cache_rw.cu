@@ -170,7 +170,13 @@ __device__ __forceinline__ uint4 take8(uint2 x, uint32_t scale) {
   uint32_t y[4];
   e4m3x4_to_f16(x.x, y[0], y[1]);
   e4m3x4_to_f16(x.y, y[2], y[3]);
-  return scaled(y, scale);
+  uint4 r = scaled(y, scale);
+  const uint32_t n0 = e4m3_nan(x.x), n1 = e4m3_nan(x.y);
+  if (n0 | n1) {      // (fp16's NaN is a finite number where its bits are moved; hga_cache_write makes none)
+    r.x |= nan_halves(n0, false); r.y |= nan_halves(n0, true);
+    r.z |= nan_halves(n1, false); r.w |= nan_halves(n1, true);
+  }
+  return r;
 }
 __device__ __forceinline__ uint4 take8(uint32_t x, uint32_t scale) {
   uint32_t y[4];
