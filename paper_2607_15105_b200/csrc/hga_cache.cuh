@@ -83,7 +83,7 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t pair(uint32_t lo_and_hi) { return lo_and_hi | (lo_and_hi << 16); }
 
 // Two e4m3 numbers, in the high bytes of the two halves (low bytes zero), as bf16 times 2^-120: sign kept, exponent and mantissa moved to
-// where bf16 has them.  Subnormal ones too: the exponent fields are both zero.
+// where bf16 has them.  Subnormal ones too: the exponent fields are both zero.  (NaN: 480 times 2^-120, see nan_halves.)
 __device__ __forceinline__ uint32_t e4m3_to_bf16_scaled(uint32_t x) {
   return (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u);
 }

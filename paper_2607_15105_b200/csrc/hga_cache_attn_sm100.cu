@@ -758,6 +758,9 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
                   if (FMT == kCacheMx8) {
                     o[k * kPairs] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x1404)), kTwo120), mul);
                     o[k * kPairs + 1] = mul_bf16x2(mul_bf16x2(e4m3_to_bf16_scaled(__byte_perm(q[k], 0, 0x3424)), kTwo120), mul);
+                    const uint32_t nan = e4m3_nan(q[k]);
+                    o[k * kPairs] |= nan_halves(nan, false);
+                    o[k * kPairs + 1] |= nan_halves(nan, true);
                   } else {
                     e2m1x4_to_bf16(q[k] & 0xffffu, o[k * kPairs], o[k * kPairs + 1]);
                     e2m1x4_to_bf16(q[k] >> 16, o[k * kPairs + 2 % kPairs], o[k * kPairs + 3 % kPairs]);

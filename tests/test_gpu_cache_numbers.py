@@ -44,3 +44,47 @@ def test_any_byte_reads_back_as_the_type_says(fmt, d):
             assert (got[:, n:] == 9).all()
 
 
+ROWS, CHUNKS = ([(6, 50), (4, 300)], 2), ([(100, 140), (64, 64)], 4)      # (sequences, query heads): the kernel for few rows, the one for chunks
+
+
+def out_of_fp16(pr):
+    """the first block of V of every sequence's first token far below fp16's range: the step, or the unit, is multiplied as bf16"""
+    for i in range(len(pr.seqs)):
+        page = int(pr.table[i, 0])
+        pr.V_scale[page, :, 0, 0] -= 60
+
+
+def check_rows(pr, Q, O, LSE, rows):
+    """these rows against 64 bits: NaN where it is NaN there, within the tolerances of Problem.attend elsewhere"""
+    want, lse, tol, tol_l = pr.attend(Q)
+    got, l = T.f64(O)[rows], T.f64(LSE)[rows]
+    nan = np.isnan(want[rows])
+    assert np.array_equal(np.isnan(got), nan)
+    assert (np.abs(got - want[rows])[~nan] <= tol[rows][~nan]).all()
+    fine = ~np.isnan(lse[rows])
+    assert np.array_equal(~np.isnan(l), fine)
+    assert (np.abs(l - lse[rows])[fine] <= tol_l[rows][fine]).all()
+    return nan
+
+
+@pytest.mark.parametrize("seqs,hq", (ROWS, CHUNKS))
+@pytest.mark.parametrize("as_bf16", (False, True))
+@pytest.mark.parametrize("name", "KV")
+def test_nan_codes_that_rows_see(seqs, hq, as_bf16, name):
+    """in the history, which all rows see: of V they make their columns NaN, of K everything"""
+    pr = Pool(seqs, "mx8", hq=hq, hkv=1, d=64, seed=42)
+    if as_bf16:
+        out_of_fp16(pr)
+    for i, (n, t) in enumerate(seqs):
+        if t > n:
+            pos = (t - n) // 2
+            page = int(pr.table[i, pos // pr.page])
+            getattr(pr, name)[page, :, pos % pr.page, 3::7] = 0x7f
+            getattr(pr, name)[page, :, pos % pr.page, 5::9] = 0xff
+    Q = pr.randn(pr.n_tokens, hq, 64)
+    O, LSE = pr.run_attn(Q.cuda())
+    nan = check_rows(pr, Q, O, LSE, slice(0, seqs[0][0]))
+    assert nan.any() and nan.all() == (name == "K")
+    assert int(pr.status.item()) == 0
+
+
