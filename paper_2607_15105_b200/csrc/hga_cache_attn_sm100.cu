@@ -9,7 +9,7 @@
 //
 //   warps 0-3, 4-7   softmax and epilogue of M-tile 0 and 1
 //   warps 8, 9       issue the GEMMs of M-tile 0 and 1
-//   warps 10, 11     copy K and V tiles by TMA, a box per page part (quantised pages: as they are, and their scales)
+//   warps 10, 11     copy K and V tiles by TMA, a box per page part (quantised pages: as they are, and their scales); e4m3: clean the last V tiles
 //   warps 12-15      bf16 pages: clean the last V tiles; quantised: convert K and V tiles
 //
 // Quantised pages are multiplied as fp16, into which the converter instructions go and which holds e4m3 and e2m1 with their scales
@@ -60,7 +60,7 @@ struct Smem {
   uint8_t ring[kSlots][kTileBytes];        // K and V tiles in turn
   uint8_t raw[2][kScaled ? kRaw + kRawScales : 128];      // quantised tiles as they lie in their pages, rows one behind the other, and their scales
   uint64_t full[kSlots], empty[kSlots];    // full: one arrival of each of the filling warps (four for the copying ones)
-  uint64_t raw_full[kSlots];               // what has to be converted has arrived (two); a V tile that has to be cleaned (any slot)
+  uint64_t raw_full[kSlots];               // K or V to be converted is there (0, 1), e4m3 V to be cleaned first (2); bf16 V to be cleaned (any slot)
   uint64_t raw_empty[2];
   // s_full, p_full: of M-tile x's buffer b.  s_full for the t-th time: S of step 2 t + b is there, if there is such a step, and P V of
   // step 2 t + b - 2 done.
@@ -354,7 +354,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
     } else {
       uint8_t* dst = sm.raw[is_v];
-      uint64_t* bar = &sm.raw_full[is_v];
+      uint64_t* bar = &sm.raw_full[FMT == kCacheMx8 && is_v && j >= first_dirty ? 2 : is_v];
       if (!all_wait(&sm.raw_empty[is_v], (j & 1) ^ 1, abort)) return false;
       if (lane == 0) mbar_arrive_expect_tx(bar, Sm::kRaw + Sm::kRawScales);
       __syncwarp();
@@ -367,6 +367,27 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
     }
     __syncwarp();
+    return true;
+  };
+  // e4m3: NaN codes in V tile j that only some rows of the unit see become zeros, by the warp that copied it.  (The converting warps, which
+  // have no registers to spare, took 6 to 34 us longer for a pass of 560 with this among their work.)
+  auto clean_tile = [&](int j) {
+    const int from = max(first_lim + 1 - (k0 + j * kTile), 0), to = min(k1 - (k0 + j * kTile), kTile);
+    constexpr int kPieces = cache_row_bytes(FMT, D) / 16;
+    if (!all_wait(&sm.raw_full[2], (j - first_dirty) & 1, abort)) return false;
+#pragma unroll 4
+    for (int i = from * kPieces + lane; i < to * kPieces; i += 32) {
+      uint4* const at16 = reinterpret_cast<uint4*>(sm.raw[1]) + i;
+      uint4 y = *at16;
+      if (e4m3_nan(y.x) | e4m3_nan(y.y) | e4m3_nan(y.z) | e4m3_nan(y.w)) {
+        uint32_t* e = &y.x;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] &= ~((e4m3_nan(e[k]) >> 7) * 255u);
+        *at16 = y;
+        sm.strange = 1;
+      }
+    }
+    mbar_arrive_warp(&sm.raw_full[1]);
     return true;
   };
   if (warp == 8) {
@@ -543,6 +564,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
         if (sm.strange && real) {
           const int end = min(lim + 1, k1);
+          uint32_t nan = 0;                                  // of a quantised pool: a bit per column
           for (int key = max(first_lim + 1, k0); key < end; ++key) {
             const int e0 = dm.by_page(key), pr = key - e0 * dm.page, page = table[seq * dm.table_stride + e0];
             if (page < 0 || page >= dm.n_pages) continue;
@@ -551,11 +573,18 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
               for (int e = 0; e < 32; ++e)
                 if (not_finite(src[e])) o[e] = __float_as_uint(__uint_as_float(o[e]) + __uint_as_float((uint32_t)src[e] << 16));
-            } else if (V_scale[(((int64_t)page * dm.Hkv + h) * dm.page + pr) * (D / 32) + (c >> 5)] == 255) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = 0x7fc00000u;
+            } else {
+              if (V_scale[(((int64_t)page * dm.Hkv + h) * dm.page + pr) * (D / 32) + (c >> 5)] == 255) nan = ~0u;
+              if (FMT == kCacheMx8) {
+                const uint8_t* src = V + page * dm.vs[0] + h * dm.vs[1] + pr * dm.vs[2] + c;
+#pragma unroll 1
+                for (int e = 0; e < 32; ++e) nan |= (src[e] & 127) == 127 ? 1u << e : 0u;
+              }
             }
           }
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if ((nan >> e) & 1) o[e] = 0x7fc00000u;
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
@@ -661,8 +690,10 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
       } else {
         // ---------------------------------------------------------------- copies (tile 0 went ahead)
-        for (int j = f16 == kScaled ? 1 : 0; j < n_tiles; ++j)
-          if (!copy_tile(j)) break;
+        for (int j = 0; j < n_tiles; ++j) {
+          if ((j > 0 || f16 != kScaled) && !copy_tile(j)) break;
+          if (FMT == kCacheMx8 && warp == 11 && j >= first_dirty && !clean_tile(j)) break;
+        }
         if (bad_page) cache_status(status_word, HGA_STATUS_BAD_INDEX);
         if (*abort && lane == 0) {
           // giving up: give the copies still in flight time to land before shared memory is released

@@ -171,7 +171,7 @@ __device__ __forceinline__ int column(int g, int t, int half) {
 template <int FMT>
 __device__ float strange_value(const uint8_t* row, const uint8_t* scale, int e) {
   if (FMT == kCacheBf16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[e] << 16);
-  return scale[e >> 5] == 255 ? __uint_as_float(0x7fc00000u) : 0.f;
+  return scale[e >> 5] == 255 || (FMT == kCacheMx8 && (row[e] & 127) == 127) ? __uint_as_float(0x7fc00000u) : 0.f;
 }
 
 template <int FMT, int D, int NT>
@@ -390,9 +390,10 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
       else *reinterpret_cast<float2*>(k_factor + lane * 2) = make_float2(f[0], f[1]);
       fits = __all_sync(0xffffffffu, fits);
       __syncwarp();
-    } else if (masked) {
-      // Values hidden from the first row: a weight of zero does not silence an infinity, so such numbers are left out here and given
-      // to the rows that see them at the end.
+    }
+    if (FMT != kCacheMx4 && masked && first_lim + 1 < k1) {
+      // Values that only some of the rows see: a weight of zero does not silence an infinity or a NaN, so such numbers are left out here and
+      // given to the rows that see them at the end.  (Scales of 255: below.  From k1 on there are zeros.)
       for (int i = lane; i < KS * Rg::NP; i += 32) {
         const int r = i / Rg::NP;
         if (base + r <= first_lim) continue;
@@ -402,8 +403,14 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
         bool odd = false;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          if ((w[k] & 0x7f80u) == 0x7f80u) { w[k] &= 0xffff0000u; odd = true; }
-          if ((w[k] & 0x7f800000u) == 0x7f800000u) { w[k] &= 0xffffu; odd = true; }
+          if (FMT == kCacheMx8) {
+            const uint32_t nan = e4m3_nan(w[k]);
+            w[k] &= ~((nan >> 7) * 255u);
+            odd = odd || nan;
+          } else {
+            if ((w[k] & 0x7f80u) == 0x7f80u) { w[k] &= 0xffff0000u; odd = true; }
+            if ((w[k] & 0x7f800000u) == 0x7f800000u) { w[k] &= 0xffffu; odd = true; }
+          }
         }
         if (odd) { *y = x; strange = true; }
       }

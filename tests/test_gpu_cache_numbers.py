@@ -88,3 +88,33 @@ def test_nan_codes_that_rows_see(seqs, hq, as_bf16, name):
     assert int(pr.status.item()) == 0
 
 
+@pytest.mark.parametrize("seqs,hq", (ROWS, CHUNKS))
+@pytest.mark.parametrize("as_bf16", (False, True))
+def test_nan_codes_that_rows_do_not_see(seqs, hq, as_bf16):
+    """in newer tokens, in the rest of the last page and in pages of nobody: rows ahead of them are what they would be"""
+    pr = Pool(seqs, "mx8", hq=hq, hkv=1, d=64, seed=43)
+    if as_bf16:
+        out_of_fp16(pr)
+    used = {(int(pr.table[i, x // pr.page]), x % pr.page) for i, (_, t) in enumerate(seqs) for x in range(t)}
+    for page in range(pr.n_pages):
+        for r in range(pr.page):
+            if (page, r) not in used:
+                pr.K[page, :, r] = pr.V[page, :, r] = 0x7f
+    slots = {row: (page, r) for row, page, r in pr.new_slots()}
+    for i, (n, t) in enumerate(seqs):
+        page, r = slots[int(pr.cu[i]) + 2]
+        pr.V[page, :, r, 3::7] = 0x7f
+        pr.V[page, :, r, 5::9] = 0xff
+        page, r = slots[int(pr.cu[i]) + n - 1]
+        pr.K[page, :, r, 11] = 0xff
+    Q = pr.randn(pr.n_tokens, hq, 64)
+    O, LSE = pr.run_attn(Q.cuda())
+    nan = check_rows(pr, Q, O, LSE, slice(None))
+    for i, (n, t) in enumerate(seqs):
+        a = int(pr.cu[i])
+        assert not nan[a:a + 2].any()
+        assert nan[a + 2:a + n - 1].any(-1).all() and not nan[a + 2:a + n - 1].all()
+        assert nan[a + n - 1].all()
+    assert int(pr.status.item()) == 0
+
+
