@@ -371,6 +371,7 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
         wk = *reinterpret_cast<const uint16_t*>(sc + lane * 2);
         wv = *reinterpret_cast<const uint16_t*>(sc + KS * NB + lane * 2);
       }
+      if (base + lane >= k1) wv = 0x7f7f7f7fu;      // (what lies behind the last key, numbers that are zeros here, does not decide how a step is multiplied)
       float f[NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b) {

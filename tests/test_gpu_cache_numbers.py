@@ -118,3 +118,58 @@ def test_nan_codes_that_rows_do_not_see(seqs, hq, as_bf16):
     assert int(pr.status.item()) == 0
 
 
+@pytest.mark.parametrize("fmt", ("mx8", "mx4"))
+@pytest.mark.parametrize("seqs,hq", (([(1, 27), (1, 95), (2, 31), (1, 300), (1, 5)], 4), ([(70, 91), (90, 125), (64, 64), (3, 30)], 4)))
+def test_slots_behind_a_sequence_change_no_bit(fmt, seqs, hq):
+    """whatever the page's owner before left there, scales that fp16 does not hold among it"""
+    pr = T.Problem(seqs, fmt, hq=hq, hkv=1, d=64, seed=44)
+    Q = pr.randn(pr.n_tokens, hq, 64).cuda()
+    used = torch.zeros(pr.n_pages, pr.page, dtype=torch.bool)
+    for i, (_, t) in enumerate(seqs):
+        for x in range(t):
+            used[int(pr.table[i, x // pr.page]), x % pr.page] = True
+    free = (~used).cuda()[:, None, :, None]
+    first = pr.run_attn(Q)
+    for scale in (127, 0, 60, 200, 255):
+        for t in (pr.K, pr.V):
+            t.copy_(torch.where(free, torch.randint(0, 256, t.shape, generator=pr.g).to(torch.uint8).cuda(), t))
+        for t in (pr.K_scale, pr.V_scale):
+            t.copy_(torch.where(free, torch.full_like(t, scale), t))
+        for a, b in zip(first, pr.run_attn(Q)):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16)), scale
+
+
+@pytest.mark.parametrize("fmt", ("mx8", "mx4"))
+@pytest.mark.parametrize("new,lengths,hq", ((1, (2, 3, 5, 7, 8, 13, 17, 24, 33, 40, 50), 8), (13, (13, 14, 21, 40), 8)))
+@pytest.mark.parametrize("what", ("lengths",))
+def test_weights_over_quantised_pages_are_fp16(fmt, new, lengths, hq, what):
+    """where the scales of the values are in fp16's range: also in the last few keys of a sequence, beside blocks of zeros, and beside pages that are none.
+
+    Values of one size and either sign: O is a difference of weights, so their rounding shows.  Off by 2^-11 of themselves and 2^-31 of the row's
+    largest they move O, which is divided by the sum of the rounded ones, by 2^-11 (a + |O|) + 2^-30 n at most, a = sum w |v|; its own rounding adds 2^-8
+    |O|; logits, exp2 (2^-18.5) and sums as in Problem.attend."""
+    pr = T.Problem([(new, t) for t in lengths], fmt, hq=hq, hkv=1, d=64, page=8, seed=45)
+    pr.V.copy_(torch.where(pr.V >= 128, 0xb8, 0x38) if fmt == "mx8" else (pr.V & 0x88) | 0x22)      # +-1
+    pr.V_scale.fill_(127)
+    if what == "zeros":
+        zero = torch.rand(pr.V_scale.shape, generator=pr.g) < 0.3
+        pr.V_scale[zero.cuda()] = 0
+        pr.V.view(*pr.V_scale.shape, -1)[zero.cuda()] = 0
+    if what == "no page":
+        pr.table[:, 0] = -1
+        pr.d_table = pr.table.cuda()
+    Q = pr.randn(pr.n_tokens, hq, 64)
+    O, LSE = pr.run_attn(Q.cuda())
+    want, lse, _, _ = pr.attend(Q)
+    Kv, Vv = pr.values("K"), pr.values("V")
+    for i, t in enumerate(lengths):
+        K, V = pr.resident(Kv, i)[0], pr.resident(Vv, i)[0]
+        for j in range(new):
+            row, end = i * new + j, t - new + j + 1
+            q = T.f64(Q[row])
+            a = np.exp(q @ K[:end].T / 8 - lse[row][:, None]) @ np.abs(V[:end])
+            off = 68 * 2.0 ** -23 * (np.abs(q) @ np.abs(K[:end]).T / 8).max() + 2.0 ** -18.5 + 2.0 ** -23 * end
+            tol = 2.0 ** -11 * (a + np.abs(want[row])) + 2.0 ** -30 * end + 2.0 ** -8 * np.abs(want[row]) + 2 * off * (a + np.abs(want[row]))
+            assert (np.abs(T.f64(O[row]) - want[row]) <= tol).all()
+
+
