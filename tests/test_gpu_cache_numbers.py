@@ -141,7 +141,7 @@ def test_slots_behind_a_sequence_change_no_bit(fmt, seqs, hq):
 
 @pytest.mark.parametrize("fmt", ("mx8", "mx4"))
 @pytest.mark.parametrize("new,lengths,hq", ((1, (2, 3, 5, 7, 8, 13, 17, 24, 33, 40, 50), 8), (13, (13, 14, 21, 40), 8)))
-@pytest.mark.parametrize("what", ("lengths",))
+@pytest.mark.parametrize("what", ("lengths", "zeros", "no page"))
 def test_weights_over_quantised_pages_are_fp16(fmt, new, lengths, hq, what):
     """where the scales of the values are in fp16's range: also in the last few keys of a sequence, beside blocks of zeros, and beside pages that are none.
 
