@@ -310,7 +310,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
           for (int k = 0; k < 4; ++k) big = max(big, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
 #pragma unroll
           for (int k = 1; k < C; k <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, k));
-          const int up = max(min(127 + 14 - (int)(big >> 7), 100), -100);
+          const int up = max(min(127 + 14 - (int)(big >> 7), 100), -113);
           const float f = __uint_as_float((uint32_t)(127 + up) << 23);
           if (c == 0) sm.q_up[row] = (int8_t)up;
 #pragma unroll

@@ -274,7 +274,7 @@ k_cache_rows(const CacheDims dm, const CacheSplit sp, int n_mt, const uint16_t* 
       big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
       big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
       // the row's largest to 2^14 .. 2^15, by a power of two that fp32 holds (and its inverse)
-      const int up = max(min(127 + 14 - (int)(big >> 7), 100), -100);
+      const int up = max(min(127 + 14 - (int)(big >> 7), 100), -113);
       const float f = __uint_as_float((uint32_t)(127 + up) << 23);
       per_row *= __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll

@@ -173,3 +173,21 @@ def test_weights_over_quantised_pages_are_fp16(fmt, new, lengths, hq, what):
             assert (np.abs(T.f64(O[row]) - want[row]) <= tol).all()
 
 
+@pytest.mark.parametrize("fmt", ("mx8", "mx4"))
+@pytest.mark.parametrize("seqs,hq", (ROWS, CHUNKS))
+@pytest.mark.parametrize("up", (110, 116, 118, 122))
+@pytest.mark.parametrize("small_keys", (False, True))
+def test_queries_next_to_the_end_of_bf16(fmt, seqs, hq, up, small_keys):
+    """logits are of ordinary size by softmax_scale, or by it and keys that are small in turn (none below 2^-118)"""
+    pr = T.Problem(seqs, fmt, hq=hq, hkv=1, d=64, seed=46)
+    Q = (pr.randn(pr.n_tokens, hq, 64).float() * 2.0 ** up).bfloat16()
+    assert torch.isfinite(Q).all()
+    down = min(up, 100 if fmt == "mx8" else 114) if small_keys else 0
+    pr.K_scale -= down
+    scale = pr.p.softmax_scale = 2.0 ** (down - up - 3)
+    O, LSE = pr.run_attn(Q.cuda())
+    want, lse, tol, tol_l = pr.attend(Q, scale)
+    assert (np.abs(T.f64(O) - want) <= tol).all() and (np.abs(T.f64(LSE) - lse) <= tol_l).all()
+    assert tol.max() < 0.1 and int(pr.status.item()) == 0
+
+
