@@ -25,9 +25,11 @@ __device__ inline uint16_t f64_to_bf16_once(double x) {
 // CTA has warps).  A warp's 32 lanes cover 32 / (D/8) consecutive rows per load instruction, 16 bytes per
 // lane, and request up to four such row sets before the first sum: the kernel is one round trip to memory
 // deep, which is what bounds a 4 MB stream spread over the whole GPU.
+// (K is not __restrict__: it may be what hga_cache_read, the call before, is still writing, and loads through such a pointer could be moved
+// ahead of griddepcontrol.wait.)
 template <int D, class Segs>
 __global__ void __launch_bounds__(256, 3)
-k_build_summaries(const uint16_t* __restrict__ K, const Dims dm, int chunk_begin,
+k_build_summaries(const uint16_t* K, const Dims dm, int chunk_begin,
                   uint16_t* __restrict__ chunk_sum, uint16_t* __restrict__ group_sum, const __grid_constant__ Segs segs) {
   constexpr int VEC = D / 8;                  // lanes across one row
   constexpr int RPI = 32 / VEC;               // rows per load instruction

@@ -191,3 +191,38 @@ def test_queries_next_to_the_end_of_bf16(fmt, seqs, hq, up, small_keys):
     assert tol.max() < 0.1 and int(pr.status.item()) == 0
 
 
+@pytest.mark.parametrize("fmt", ("bf16", "mx8", "mx4"))
+def test_summaries_straight_behind_a_read_back(fmt):
+    """write, read back and summaries one straight behind the other, with other contents every time, against the same calls with a wait after each"""
+    from paper_2607_15105_b200.workloads import HgaConfig
+    hkv, d, total, n = 2, 128, 512, 24
+    cfg = HgaConfig("cache", batch=2, n_q_heads=4, n_kv_heads=hkv, head_dim=d, total_len=total, seg_len=64, chunk=64, group=8, q_block=64,
+                    topk_chunks=2, topk_groups=2, sink=64, local=64, topics=4, needles=0, backward=False, seed=1)
+    pr = T.Problem([(total, total), (total, total)], fmt, hq=4, hkv=hkv, d=d, page=64, seed=51)
+    new = pr.randn(n, 2 * total, hkv, d).cuda()
+    bufs = [[binding.HgaLayerBuffers(cfg, backward=False) for _ in range(n)] for _ in range(2)]
+    dense = torch.zeros(2, hkv, total, d, dtype=torch.bfloat16, device="cuda")
+
+    def step(i, buf, wait):
+        binding.hga_cache_write(pr.p, new[i], None, pr.d_cu, pr.d_lens, pr.d_table, pr.K, None, pr.K_scale, None, pr.status)
+        wait()
+        binding.hga_cache_read(pr.p, 0, total, pr.d_lens, pr.d_table, pr.K, None, pr.K_scale, None, dense, None, pr.status)
+        wait()
+        buf.build_summaries(dense, 0, total)
+        wait()
+
+    torch.cuda.synchronize()
+    for i in range(n):
+        step(i, bufs[0][i], lambda: None)
+    torch.cuda.synchronize()
+    for i in range(n):
+        step(i, bufs[1][i], torch.cuda.synchronize)
+    for a, b in zip(*bufs):
+        assert torch.equal(a.chunk_sum.view(torch.int16), b.chunk_sum.view(torch.int16)) and a.chunk_sum.abs().max() > 0
+        assert torch.equal(a.group_sum.view(torch.int16), b.group_sum.view(torch.int16))
+    # the mean of what is held, rounded once
+    k = T.f64(dense).reshape(2, hkv, total // 8, 8, d).mean(3)
+    assert (np.abs(T.f64(bufs[1][n - 1].group_sum) - k) <= 2.0 ** -8 * np.abs(k)).all()
+    assert int(pr.status.item()) == 0
+
+
