@@ -323,6 +323,12 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
   };
   // first tile with keys hidden from the unit's first row
   const int first_dirty = max(first_lim + 1 - k0, 0) / kTile;
+  // bf16: the cleaning warps have nothing to do until that tile's turn, which may be longer than a bounded wait lasts (some 10^7 keys).  The warp
+  // that copies V meets them at a barrier then, or where it gives up.
+  const bool cleaners_sleep = FMT == kCacheBf16 && first_dirty > 0 && first_dirty < n_tiles;
+  constexpr int kMeet = (kFill + 1) * 32;
+  auto barrier_arrive = [&]() { __syncwarp(); asm volatile("bar.arrive 1, %0;" ::"n"(kMeet) : "memory"); };
+  auto barrier_sync = [&]() { __syncwarp(); asm volatile("bar.sync 1, %0;" ::"n"(kMeet) : "memory"); };
   // Copies of tile j: of K by warp 10, of V by warp 11.  False: a wait ran out.
   bool bad_page = false;
   auto copy_tile = [&](int j) {
@@ -690,10 +696,13 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
       } else {
         // ---------------------------------------------------------------- copies (tile 0 went ahead)
+        bool told = warp != 11 || !cleaners_sleep;
         for (int j = 0; j < n_tiles; ++j) {
+          if (!told && j == first_dirty) { barrier_arrive(); told = true; }
           if ((j > 0 || f16 != kScaled) && !copy_tile(j)) break;
           if (FMT == kCacheMx8 && warp == 11 && j >= first_dirty && !clean_tile(j)) break;
         }
+        if (!told) barrier_arrive();
         if (bad_page) cache_status(status_word, HGA_STATUS_BAD_INDEX);
         if (*abort && lane == 0) {
           // giving up: give the copies still in flight time to land before shared memory is released
@@ -710,6 +719,7 @@ k_cache_attn_sm100(const __grid_constant__ CUtensorMap map_k, const __grid_const
         // ---------------------------------------------------------------- V tiles with hidden keys: a thread per key
         const int r = tid & 127;
         uint32_t parity = 0;                     // of each slot's raw_full
+        if (cleaners_sleep) barrier_sync();
 #pragma unroll 1
         for (int j = first_dirty; j < n_tiles; ++j) {
           const int slot = (2 * j + 1) % NS;

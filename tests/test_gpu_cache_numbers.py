@@ -226,3 +226,38 @@ def test_summaries_straight_behind_a_read_back(fmt):
     assert int(pr.status.item()) == 0
 
 
+def test_a_unit_that_takes_longer_than_a_bounded_wait():
+    """1.7 10^8 keys in one unit: all but the last 4096 are the same page, with next to no weight, so only those count"""
+    heads, page, d, new, pages = 148, 4096, 64, 64, 40960
+    g = torch.Generator(device="cuda").manual_seed(52)
+    K, V = (torch.randn(2, heads, page, d, generator=g, device="cuda").bfloat16() for _ in "KV")
+    K[0], V[0] = -8, 0                                                       # logits near -64, against -5 to 5
+    Q = (1 + 0.1 * torch.randn(new, heads, d, generator=g, device="cuda")).bfloat16()
+    table = torch.zeros(1, pages, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    p = binding.make_cache_params(1, heads, heads, d, page, 2, pages, binding.HGA_CACHE_BF16, new, new)
+    assert binding.hga_cache_workspace_bytes(p) == 0                         # (no unit is shared out)
+    cu, lens = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, new], [pages * page]))
+    O, LSE = torch.zeros_like(Q), torch.zeros(new, heads, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    binding.hga_cache_attn(p, Q, cu, lens, table, K, V, None, None, O, LSE, None, status)
+    end.record()
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    assert start.elapsed_time(end) > 1000 * 2 ** 30 / 1.965e9                # longer than the waits' 2^30 cycles
+    hidden = torch.arange(page, device="cuda")[None] > page - new + torch.arange(new, device="cuda")[:, None]
+    for h in range(0, heads, 37):
+        q, k, v = Q[:, h].double(), K[1, h].double(), V[1, h].double()
+        x = (q @ k.T / 8).masked_fill(hidden, -np.inf)
+        lse = torch.logsumexp(x, -1)
+        w = torch.exp(x - lse[:, None])
+        want, a = w @ v, w @ v.abs()
+        off = 68 * 2.0 ** -23 * (q.abs() @ k.abs().T / 8).amax(-1) + 2.0 ** -18.5
+        # (as Problem.attend; the pages before add exp(-59) 1.7 10^8 < 2^-57 to a weight of one)
+        tol = 2.0 ** -8 * (a + 2 * want.abs()) + 2 * (off + 2.0 ** -23 * 4096)[:, None] * (a + want.abs())
+        assert ((O[:, h].double() - want).abs() <= tol).all()
+        assert ((LSE[:, h].double() - lse).abs() <= 2 * off + 2.0 ** -23 * 4096 + 2.0 ** -22 * lse.abs()).all()
+
+
