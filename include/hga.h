@@ -324,7 +324,8 @@ HGA_API int hga_varlen_workspace_bytes(const hga_params* p, int32_t n_seq, const
  *   block_table  int32 [n_seq, max_pages] (rows table_stride apart)
  * Values that break these rules, or the limits max_new and max_len, fault nothing: HGA_STATUS_BAD_INDEX is set, and what lies outside
  * the limits is left out.  An entry of block_table that is used and no page of the pool counts as a page of zeros; nothing is written
- * to it.  A page that hga_cache_write writes to belongs to one sequence; pages that are only read may be shared. */
+ * to it.  A page that hga_cache_write writes to belongs to one sequence; pages that are only read may be shared.
+ * A call without new tokens (n_tokens = 0), or of an empty range of tokens, does nothing; its tensors of no rows may be NULL. */
 #define HGA_CACHE_BF16 0
 #define HGA_CACHE_MXFP8 1
 #define HGA_CACHE_MXFP4 2

@@ -93,7 +93,7 @@ int hga_cache_write(const hga_cache_params* p, const void* K_new, const void* V_
   const int rc = resolve_cache(p, dm);
   if (rc) return rc;
   const bool scaled = dm.format != HGA_CACHE_BF16;
-  if ((!K_new && !V_new) || !cu_q || !seq_lens || !block_table) return HGA_ERR_NULL;
+  if ((dm.n_tokens > 0 && !K_new && !V_new) || !cu_q || !seq_lens || !block_table) return HGA_ERR_NULL;      // (a tensor of no rows may have no address)
   if ((K_new && (!K_cache || (scaled && !K_scale))) || (V_new && (!V_cache || (scaled && !V_scale)))) return HGA_ERR_NULL;
   if (misaligned(K_new) || misaligned(V_new) || misaligned(K_cache) || misaligned(V_cache) || misaligned(K_scale) || misaligned(V_scale) ||
       misaligned(cu_q, 4) || misaligned(seq_lens, 4) || misaligned(block_table, 4))
@@ -110,7 +110,7 @@ int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t tok_end
   int rc = resolve_cache(p, dm);
   if (rc) return rc;
   const bool scaled = dm.format != HGA_CACHE_BF16;
-  if ((!K_out && !V_out) || !seq_lens || !block_table) return HGA_ERR_NULL;
+  if ((tok_end > tok_begin && !K_out && !V_out) || !seq_lens || !block_table) return HGA_ERR_NULL;
   if ((K_out && (!K_cache || (scaled && !K_scale))) || (V_out && (!V_cache || (scaled && !V_scale)))) return HGA_ERR_NULL;
   if (misaligned(K_out) || misaligned(V_out) || misaligned(K_cache) || misaligned(V_cache) || misaligned(K_scale) || misaligned(V_scale) ||
       misaligned(seq_lens, 4) || misaligned(block_table, 4))
@@ -131,7 +131,7 @@ int hga_cache_attn(const hga_cache_params* p, const void* Q, const int32_t* cu_q
   CacheDims dm;
   const int rc = resolve_cache(p, dm);
   if (rc) return rc;
-  if (!Q || !cu_q || !seq_lens || !block_table || !K_cache || !V_cache || !O) return HGA_ERR_NULL;
+  if ((dm.n_tokens > 0 && (!Q || !O)) || !cu_q || !seq_lens || !block_table || !K_cache || !V_cache) return HGA_ERR_NULL;
   if (dm.format != HGA_CACHE_BF16 && (!K_scale || !V_scale)) return HGA_ERR_NULL;
   if (misaligned(Q) || misaligned(K_cache) || misaligned(V_cache) || misaligned(K_scale) || misaligned(V_scale) || misaligned(O) ||
       misaligned(LSE, 4) || misaligned(cu_q, 4) || misaligned(seq_lens, 4) || misaligned(block_table, 4))
