@@ -379,34 +379,59 @@ def hga_cache_workspace_bytes(p: HgaCacheParams) -> int:
     return n.value
 
 
-def _check_device(call, t):
-    """The pool lies on the current device, whose stream the call goes to."""
-    if isinstance(t, torch.Tensor) and t.get_device() != torch.cuda.current_device():
-        raise ValueError("%s: the cache is on %s, the current device is cuda:%d" % (call, t.device, torch.cuda.current_device()))
+def _cache_addresses(call, tensors):
+    """The addresses of a cache call's arguments: tensors on the current device, to whose stream the call goes; or addresses, or None.
+    (hga_cache_write and hga_cache_attn have the usual case written out: the same questions, without the loop's microsecond.)"""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.get_device() != device:
+            raise ValueError("%s: an argument is on %s, the current device is cuda:%d" % (call, t.device, device))
+    return [_ptr(t) for t in tensors]
 
 
 def hga_cache_write(p, K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale=None, V_scale=None, status_word=None,
                     stream=None):
     """Keys and values of the new tokens into the paged cache (see hga.h)."""
-    _check_device("hga_cache_write", V_cache if K_cache is None else K_cache)
-    _check("hga_cache_write", lib().hga_cache_write(
-        C.byref(p), _ptr(K_new), _ptr(V_new), _ptr(cu_q), _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache),
-        _ptr(K_scale), _ptr(V_scale), _ptr(status_word), _stream(stream)))
+    try:
+        device = K_cache.get_device()
+        usual = (0 <= device == torch._C._cuda_getDevice() == V_cache.get_device() == K_new.get_device() == V_new.get_device()
+                 == cu_q.get_device() == seq_lens.get_device() == block_table.get_device() == status_word.get_device()
+                 and (K_scale is None or device == K_scale.get_device() == V_scale.get_device()))
+    except AttributeError:                          # (None, or an address)
+        usual = False
+    if usual:
+        at = (K_new.data_ptr(), V_new.data_ptr(), cu_q.data_ptr(), seq_lens.data_ptr(), block_table.data_ptr(), K_cache.data_ptr(),
+              V_cache.data_ptr(), None if K_scale is None else K_scale.data_ptr(), None if V_scale is None else V_scale.data_ptr(),
+              status_word.data_ptr())
+    else:
+        at = _cache_addresses("hga_cache_write", (
+            K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, status_word))
+    _check("hga_cache_write", lib().hga_cache_write(p, *at, _stream(stream)))
 
 
 def hga_cache_read(p, tok_begin, tok_end, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, K_out, V_out, status_word=None,
                    stream=None):
     """Resident tokens [tok_begin, tok_end) of every sequence as dense bf16 (see hga.h)."""
-    _check_device("hga_cache_read", V_cache if K_cache is None else K_cache)
-    _check("hga_cache_read", lib().hga_cache_read(
-        C.byref(p), tok_begin, tok_end, _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale),
-        _ptr(K_out), _ptr(V_out), _ptr(status_word), _stream(stream)))
+    _check("hga_cache_read", lib().hga_cache_read(p, tok_begin, tok_end, *_cache_addresses("hga_cache_read", (
+        seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, K_out, V_out, status_word)), _stream(stream)))
 
 
 def hga_cache_attn(p, Q, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, O, LSE=None, workspace=None,
                    status_word=None, stream=None):
     """Exact attention of the new tokens over the paged cache (see hga.h)."""
-    _check_device("hga_cache_attn", K_cache)
-    _check("hga_cache_attn", lib().hga_cache_attn(
-        C.byref(p), _ptr(Q), _ptr(cu_q), _ptr(seq_lens), _ptr(block_table), _ptr(K_cache), _ptr(V_cache), _ptr(K_scale), _ptr(V_scale),
-        _ptr(O), _ptr(LSE), _ptr(workspace), _nbytes(workspace), _ptr(status_word), _stream(stream)))
+    try:
+        device = K_cache.get_device()
+        usual = (0 <= device == torch._C._cuda_getDevice() == V_cache.get_device() == Q.get_device() == O.get_device() == LSE.get_device()
+                 == cu_q.get_device() == seq_lens.get_device() == block_table.get_device() == workspace.get_device() == status_word.get_device()
+                 and (K_scale is None or device == K_scale.get_device() == V_scale.get_device()))
+    except AttributeError:
+        usual = False
+    if usual:
+        at = (Q.data_ptr(), cu_q.data_ptr(), seq_lens.data_ptr(), block_table.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(),
+              None if K_scale is None else K_scale.data_ptr(), None if V_scale is None else V_scale.data_ptr(), O.data_ptr(), LSE.data_ptr(),
+              workspace.data_ptr(), workspace.nbytes, status_word.data_ptr())
+    else:
+        at = _cache_addresses("hga_cache_attn", (
+            Q, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, O, LSE, workspace, status_word))
+        at.insert(-1, _nbytes(workspace))
+    _check("hga_cache_attn", lib().hga_cache_attn(p, *at, _stream(stream)))
