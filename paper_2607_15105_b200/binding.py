@@ -379,14 +379,38 @@ def hga_cache_workspace_bytes(p: HgaCacheParams) -> int:
     return n.value
 
 
-def _cache_addresses(call, tensors):
-    """The addresses of a cache call's arguments: tensors on the current device, to whose stream the call goes; or addresses, or None.
-    (hga_cache_write and hga_cache_attn have the usual case written out: the same questions, without the loop's microsecond.)"""
+# Which strides of the parameters the arguments of a cache call go by, in the call's order; None: they have to be dense
+_WRITE_STRIDES = ("kn_stride", "vn_stride", None, None, "table_stride", "k_stride", "v_stride", None, None, None)
+_READ_STRIDES = (None, "table_stride", "k_stride", "v_stride", None, None, "out_stride", "out_stride", None)
+_ATTN_STRIDES = ("q_stride", None, None, "table_stride", "k_stride", "v_stride", None, None, "o_stride", None, None, None)
+
+
+def _cache_addresses(call, p, strides, tensors):
+    """The addresses of a cache call's arguments: tensors on the current device, to whose stream the call goes, and dense where the parameters have no
+    strides for them; or addresses, or None.  (hga_cache_write and hga_cache_attn have the usual case written out: the same questions, without the
+    loop's microsecond.)"""
     device = torch.cuda.current_device()
-    for t in tensors:
-        if isinstance(t, torch.Tensor) and t.get_device() != device:
-            raise ValueError("%s: an argument is on %s, the current device is cuda:%d" % (call, t.device, device))
-    return [_ptr(t) for t in tensors]
+    try:
+        there = [t for t in tensors if t is not None]
+        usual = set(map(torch.Tensor.get_device, there)) == {device} and all(map(torch.Tensor.is_contiguous, there))
+    except TypeError:                               # (an address)
+        usual = False
+    if not usual:
+        for t, s in zip(tensors, strides):
+            if isinstance(t, torch.Tensor):
+                _check_cache_tensor(call, device, p, s, t)
+    return [t if t is None or isinstance(t, int) else t.data_ptr() for t in tensors]
+
+
+def _check_cache_tensor(call, device, p, strides, t):
+    if t.get_device() != device:
+        raise ValueError("%s: an argument is on %s, the current device is cuda:%d" % (call, t.device, device))
+    if t.is_contiguous():
+        return
+    given = getattr(p, strides) if strides else 0
+    if t.stride(-1) != 1 or not (given if isinstance(given, int) else any(given)):
+        raise ValueError("%s: a tensor has strides %s, but %s" % (
+            call, tuple(t.stride()), "the parameters give none for it (%s), or its last axis is not dense" % strides if strides else "has to be dense"))
 
 
 def hga_cache_write(p, K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale=None, V_scale=None, status_word=None,
@@ -395,16 +419,20 @@ def hga_cache_write(p, K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cac
     try:
         device = K_cache.get_device()
         usual = (0 <= device == torch._C._cuda_getDevice() == V_cache.get_device() == K_new.get_device() == V_new.get_device()
-                 == cu_q.get_device() == seq_lens.get_device() == block_table.get_device() == status_word.get_device()
-                 and (K_scale is None or device == K_scale.get_device() == V_scale.get_device()))
+                 == cu_q.get_device() == seq_lens.get_device() == block_table.get_device()
+                 and (status_word is None or status_word.get_device() == device)
+                 and K_cache.is_contiguous() and V_cache.is_contiguous() and K_new.is_contiguous() and V_new.is_contiguous()
+                 and cu_q.is_contiguous() and seq_lens.is_contiguous() and block_table.is_contiguous()
+                 and (K_scale is None or device == K_scale.get_device() == V_scale.get_device()
+                      and K_scale.is_contiguous() and V_scale.is_contiguous()))
     except AttributeError:                          # (None, or an address)
         usual = False
     if usual:
         at = (K_new.data_ptr(), V_new.data_ptr(), cu_q.data_ptr(), seq_lens.data_ptr(), block_table.data_ptr(), K_cache.data_ptr(),
               V_cache.data_ptr(), None if K_scale is None else K_scale.data_ptr(), None if V_scale is None else V_scale.data_ptr(),
-              status_word.data_ptr())
+              None if status_word is None else status_word.data_ptr())
     else:
-        at = _cache_addresses("hga_cache_write", (
+        at = _cache_addresses("hga_cache_write", p, _WRITE_STRIDES, (
             K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, status_word))
     _check("hga_cache_write", lib().hga_cache_write(p, *at, _stream(stream)))
 
@@ -412,7 +440,7 @@ def hga_cache_write(p, K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cac
 def hga_cache_read(p, tok_begin, tok_end, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, K_out, V_out, status_word=None,
                    stream=None):
     """Resident tokens [tok_begin, tok_end) of every sequence as dense bf16 (see hga.h)."""
-    _check("hga_cache_read", lib().hga_cache_read(p, tok_begin, tok_end, *_cache_addresses("hga_cache_read", (
+    _check("hga_cache_read", lib().hga_cache_read(p, tok_begin, tok_end, *_cache_addresses("hga_cache_read", p, _READ_STRIDES, (
         seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, K_out, V_out, status_word)), _stream(stream)))
 
 
@@ -421,17 +449,22 @@ def hga_cache_attn(p, Q, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale,
     """Exact attention of the new tokens over the paged cache (see hga.h)."""
     try:
         device = K_cache.get_device()
-        usual = (0 <= device == torch._C._cuda_getDevice() == V_cache.get_device() == Q.get_device() == O.get_device() == LSE.get_device()
-                 == cu_q.get_device() == seq_lens.get_device() == block_table.get_device() == workspace.get_device() == status_word.get_device()
-                 and (K_scale is None or device == K_scale.get_device() == V_scale.get_device()))
+        usual = (0 <= device == torch._C._cuda_getDevice() == V_cache.get_device() == Q.get_device() == O.get_device()
+                 == cu_q.get_device() == seq_lens.get_device() == block_table.get_device() == workspace.get_device()
+                 and (status_word is None or status_word.get_device() == device)
+                 and (LSE is None or LSE.get_device() == device and LSE.is_contiguous())
+                 and K_cache.is_contiguous() and V_cache.is_contiguous() and Q.is_contiguous() and O.is_contiguous()
+                 and cu_q.is_contiguous() and seq_lens.is_contiguous() and block_table.is_contiguous() and workspace.is_contiguous()
+                 and (K_scale is None or device == K_scale.get_device() == V_scale.get_device()
+                      and K_scale.is_contiguous() and V_scale.is_contiguous()))
     except AttributeError:
         usual = False
     if usual:
         at = (Q.data_ptr(), cu_q.data_ptr(), seq_lens.data_ptr(), block_table.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(),
-              None if K_scale is None else K_scale.data_ptr(), None if V_scale is None else V_scale.data_ptr(), O.data_ptr(), LSE.data_ptr(),
-              workspace.data_ptr(), workspace.nbytes, status_word.data_ptr())
+              None if K_scale is None else K_scale.data_ptr(), None if V_scale is None else V_scale.data_ptr(), O.data_ptr(),
+              None if LSE is None else LSE.data_ptr(), workspace.data_ptr(), workspace.nbytes, None if status_word is None else status_word.data_ptr())
     else:
-        at = _cache_addresses("hga_cache_attn", (
+        at = _cache_addresses("hga_cache_attn", p, _ATTN_STRIDES, (
             Q, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, O, LSE, workspace, status_word))
         at.insert(-1, _nbytes(workspace))
     _check("hga_cache_attn", lib().hga_cache_attn(p, *at, _stream(stream)))

@@ -38,6 +38,21 @@ def test_any_tensor_on_the_host_is_refused(fmt):
     assert binding.hga_kernel_launch_count() == before + 9 and int(pr.status.item()) == 0
 
 
+@pytest.mark.parametrize("fmt", ("bf16", "mx8"))
+def test_tensors_that_are_not_dense_are_refused_without_their_strides(fmt):
+    pr = T.Problem([(2, 40), (1, 30)], fmt, hq=4, hkv=2, d=64, seed=62)
+    for s in (pr.p.k_stride, pr.p.v_stride):
+        s[:] = (0, 0, 0)
+    before = binding.hga_kernel_launch_count()
+    for call, args in arguments(pr).items():
+        for name, t in args.items():
+            if isinstance(t, torch.Tensor) and t.numel() > 1:
+                wide = torch.zeros(*t.shape, 2, dtype=t.dtype, device="cuda")[..., 0]
+                with pytest.raises(ValueError, match="strides"):
+                    call(pr.p, **dict(args, **{name: wide}))
+    assert binding.hga_kernel_launch_count() == before
+
+
 def test_a_step_without_tokens():
     pr = T.Problem([(0, 40), (0, 30)], "mx8", hq=4, hkv=2, d=64, seed=63)
     before = binding.hga_kernel_launch_count()
