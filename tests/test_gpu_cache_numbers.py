@@ -261,3 +261,50 @@ def test_a_unit_that_takes_longer_than_a_bounded_wait():
         assert ((LSE[:, h].double() - lse).abs() <= 2 * off + 2.0 ** -23 * 4096 + 2.0 ** -22 * lse.abs()).all()
 
 
+@pytest.mark.parametrize("fmt", ("bf16", "mx8", "mx4"))
+@pytest.mark.parametrize("seqs,hq", (([(1, 60), (2, 300), (1, 2000)], 4), ([(70, 250), (64, 64)], 4)))
+def test_values_up_to_the_stated_size(fmt, seqs, hq):
+    """keys times the largest value just below 2^108; and beyond it, in one sequence, which leaves the others as they are"""
+    pr = T.Problem(seqs, fmt, hq=hq, hkv=1, d=64, seed=47)
+    most = max(t for _, t in seqs)
+    ordinary = pr.V.clone(), None if fmt == "bf16" else pr.V_scale.clone()
+    Q = pr.randn(pr.n_tokens, hq, 64)
+    plain = pr.run_attn(Q.cuda())
+    up = int(np.floor(np.log2(2.0 ** 108 / most / np.abs(pr.values("V")).max())))
+    if fmt == "bf16":
+        pr.V.mul_(2.0 ** up)
+    else:
+        pr.V_scale += up
+    assert 2.0 ** 107 / 2 < np.abs(pr.values("V")).max() * most < 2.0 ** 108
+    O, LSE = pr.run_attn(Q.cuda())
+    pr.check_attn(Q, O, LSE)
+    pr.V.copy_(ordinary[0])
+    if fmt != "bf16":
+        pr.V_scale.copy_(ordinary[1])
+    for page in pr.table[0][pr.table[0] >= 0].tolist():
+        if fmt == "bf16":
+            pr.V[page] *= 2.0 ** 124
+        else:
+            pr.V_scale[page] += 110
+    O, LSE = pr.run_attn(Q.cuda())
+    n = seqs[0][0]
+    assert torch.equal(O[n:].view(torch.int16), plain[0][n:].view(torch.int16)) and torch.equal(LSE[n:], plain[1][n:])
+    assert int(pr.status.item()) == 0
+
+
+@pytest.mark.parametrize("fmt", ("mx8", "mx4"))
+@pytest.mark.parametrize("seqs,hq", (ROWS, CHUNKS))
+def test_keys_up_to_the_stated_size(fmt, seqs, hq):
+    """just below 2^100, against queries that are small in turn, and against ordinary ones under a small softmax_scale"""
+    pr = T.Problem(seqs, fmt, hq=hq, hkv=1, d=64, seed=53)
+    up = int(np.floor(np.log2(2.0 ** 100 / np.abs(pr.values("K")).max())))
+    pr.K_scale += up
+    for down in (up, 0):
+        Q = (pr.randn(pr.n_tokens, hq, 64).float() * 2.0 ** -down).bfloat16()
+        scale = pr.p.softmax_scale = 2.0 ** (down - up - 3)
+        O, LSE = pr.run_attn(Q.cuda())
+        want, lse, tol, tol_l = pr.attend(Q, scale)
+        assert (np.abs(T.f64(O) - want) <= tol).all() and (np.abs(T.f64(LSE) - lse) <= tol_l).all()
+    assert int(pr.status.item()) == 0
+
+
