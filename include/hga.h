@@ -367,11 +367,17 @@ HGA_API int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t
  * position pos = seq_lens[i] - (cu_q[i+1] - cu_q[i]) + (t - cu_q[i]), attends to keys 0 .. pos (query head h to key/value head
  * h / (Hq/Hkv)); hga_cache_write has put the new tokens' own keys there before.
  *   Q, O bf16 [n_tokens, Hq, d]      LSE fp32 [n_tokens, Hq] (natural log; optional, may be NULL)
- * A row that sees no key gets O = 0 and LSE = -inf.  Rows outside cu_q are left as they were.  Keys and values that a row does not
- * see have no influence on it, not even infinities or NaN.  Products are of bf16 numbers (the cache's are), sums in fp32; the
- * probabilities are rounded to bf16 (over a quantised pool to fp16: off by 2^-11 of themselves, or 2^-31 of the row's largest).  Numbers of a
- * quantised pool below 2^-118 count as zeros, and of a query row those that are below 2^-29 of its largest or 2^-125 lose bits.  O overlaps no
- * input.  Results do not depend on what else is in the batch, nor change from
+ * A row that sees no key gets O = 0 and LSE = -inf.  Rows outside cu_q are left as they were.  O overlaps no input.  Keys and values that a
+ * row does not see have no influence on it, not even infinities or NaN, but for one: newer tokens may decide how probabilities are rounded.
+ * Products are of bf16 numbers (the cache's are), sums in fp32, powers of two within 2^-18 of themselves.  Probabilities are rounded
+ *   over a bf16 pool      to bf16: off by 2^-8 of themselves
+ *   over a quantised one  to fp16: off by 2^-11 of themselves or 2^-31 of the row's largest; or to bf16 where scales of blocks that are not all
+ *                         zeros lie outside 2^-18 .. 2^1 (e4m3), 2^-16 .. 2^9 (e2m1): with up to 48 or 64 new tokens x Hq/Hkv, all with a V
+ *                         scale of that kind among the same 32 keys; with more, all of up to 256 such rows if any key up to the last one's has it in
+ *                         K or V.  (These rows are computed twice: a chunk with a scale of that kind in its history takes twice as long or more.)
+ * Numbers of a quantised pool below 2^-118 count as zeros, and of a query row over one those that are below 2^-29 of its largest or 2^-117
+ * lose bits.
+ * Results do not depend on what else is in the batch, nor change from
  * run to run, except that max_len, max_new and n_seq decide how the keys are shared out.
  * Sizes: logits (after the scale) below 2^24 in magnitude; the number of keys times the largest |V| below 2^108; in a quantised pool |K| below
  * 2^100.  Beyond these, sums may overflow: rows of that sequence may be infinite or NaN.

@@ -308,3 +308,28 @@ def test_keys_up_to_the_stated_size(fmt, seqs, hq):
     assert int(pr.status.item()) == 0
 
 
+@pytest.mark.parametrize("fmt,low,high", (("mx8", 109, 128), ("mx4", 111, 136)))
+@pytest.mark.parametrize("new,lengths", ((1, (2, 3, 5, 8, 24, 40)), (13, (13, 14, 21, 40))))
+def test_the_range_of_scales_with_fp16_weights(fmt, low, high, new, lengths):
+    """2^-18 to 2^1 in e4m3 and 2^-16 to 2^9 in e2m1, of keys and values; tolerance as in the test of that rounding"""
+    for code in (low, high):
+        pr = T.Problem([(new, t) for t in lengths], fmt, hq=8, hkv=1, d=64, page=8, seed=54)
+        pr.V.copy_(torch.where(pr.V >= 128, 0xb8, 0x38) if fmt == "mx8" else (pr.V & 0x88) | 0x22)      # +-1
+        pr.V_scale.fill_(code)
+        pr.K_scale.fill_(code)
+        size = np.abs(pr.values("K")).max()
+        Q = (pr.randn(pr.n_tokens, 8, 64).float() * (4 / size)).bfloat16()
+        O, LSE = pr.run_attn(Q.cuda())
+        want, lse, _, _ = pr.attend(Q)
+        Kv, Vv = pr.values("K"), pr.values("V")
+        for i, t in enumerate(lengths):
+            K, V = pr.resident(Kv, i)[0], pr.resident(Vv, i)[0]
+            for j in range(new):
+                row, end = i * new + j, t - new + j + 1
+                q = T.f64(Q[row])
+                a = np.exp(q @ K[:end].T / 8 - lse[row][:, None]) @ np.abs(V[:end])
+                off = 68 * 2.0 ** -23 * (np.abs(q) @ np.abs(K[:end]).T / 8).max() + 2.0 ** -18.5 + 2.0 ** -23 * end
+                tol = 2.0 ** -11 * (a + np.abs(want[row])) + 2.0 ** -30 * end * 2.0 ** (code - 127) + 2.0 ** -8 * np.abs(want[row]) + 2 * off * (a + np.abs(want[row]))
+                assert (np.abs(T.f64(O[row]) - want[row]) <= tol).all()
+
+
