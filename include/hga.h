@@ -377,8 +377,8 @@ HGA_API int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t
  *                         K or V.  (These rows are computed twice: a chunk with a scale of that kind in its history takes twice as long or more.)
  * Numbers of a quantised pool below 2^-118 count as zeros, and of a query row over one those that are below 2^-29 of its largest or 2^-117
  * lose bits.
- * Results do not depend on what else is in the batch, nor change from
- * run to run, except that max_len, max_new and n_seq decide how the keys are shared out.
+ * Results do not depend on what else is in the batch, nor change from run to run, except that the numbers in the parameters (n_seq, n_tokens,
+ * max_new, max_len and the like) decide how the keys are shared out.
  * Sizes: logits (after the scale) below 2^24 in magnitude; the number of keys times the largest |V| below 2^108; in a quantised pool |K| below
  * 2^100.  Beyond these, sums may overflow: rows of that sequence may be infinite or NaN.
  * workspace: device scratch of at least hga_cache_workspace_bytes() bytes (16-byte aligned; may be NULL where that is 0); contents

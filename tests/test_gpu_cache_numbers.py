@@ -333,3 +333,45 @@ def test_the_range_of_scales_with_fp16_weights(fmt, low, high, new, lengths):
                 assert (np.abs(T.f64(O[row]) - want[row]) <= tol).all()
 
 
+@pytest.mark.parametrize("fmt", ("bf16", "mx8", "mx4"))
+@pytest.mark.parametrize("new,length,others,hq", (
+    (1, 900, ((2, 800, 1, 300), (1, 70, 2, 7), (0, 0, 3, 1000)), 8), (1, 100, ((1, 80, 1, 90), (2, 2, 0, 50), (0, 5, 2, 100)), 8),
+    (70, 400, ((30, 390, 40, 40), (70, 90, 0, 400), (1, 1, 69, 300)), 4)))
+def test_neighbours_change_no_bit(fmt, new, length, others, hq):
+    """one sequence beside others of other lengths and contents, in another place of the batch, with the same n_seq, n_tokens, max_new and max_len"""
+    g = torch.Generator().manual_seed(48)
+    q = torch.randn(new, hq, 64, generator=g).bfloat16()
+    first = None
+    for at in (0, 1, 2):
+        for a, ta, b, tb in others:
+            seqs = [(a, ta), (b, tb)]
+            seqs.insert(at, (new, length))
+            pr = T.Problem(seqs, fmt, hq=hq, hkv=1, d=64, seed=49 + at, max_new=max(new, 3), max_len=1000)
+            table = torch.full((3, 63), -7, dtype=torch.int32)                # (the same limits every time)
+            table[:, :pr.table.shape[1]] = pr.table
+            pr.table, pr.d_table, pr.p.max_pages = table, table.cuda(), 63
+            # the sequence's own tokens, the same every time
+            own = torch.Generator().manual_seed(50)
+            for t in pr.cache():
+                if t is None:
+                    continue
+                for e in range(-(-length // pr.page)):
+                    page = int(pr.table[at, e])
+                    if t.dtype == torch.bfloat16:
+                        t[page] = torch.randn(t[page].shape, generator=own).bfloat16()
+                    elif t.shape[-1] == 2:
+                        t[page] = torch.randint(118, 124, t[page].shape, generator=own).to(torch.uint8)
+                    else:
+                        t[page] = torch.randint(0, 126, t[page].shape, generator=own).to(torch.uint8)
+            Q = pr.randn(pr.n_tokens, hq, 64)
+            row = int(pr.cu[at])
+            Q[row:row + new] = q
+            O, LSE = pr.run_attn(Q.cuda())
+            got = O[row:row + new].clone(), LSE[row:row + new].clone()
+            assert torch.isfinite(got[0]).all()
+            if first is None:
+                first = got
+            assert torch.equal(first[0].view(torch.int16), got[0].view(torch.int16)) and torch.equal(first[1], got[1]), (at, seqs)
+            assert int(pr.status.item()) == 0
+
+
