@@ -96,7 +96,7 @@ int hga_cache_write(const hga_cache_params* p, const void* K_new, const void* V_
   if ((dm.n_tokens > 0 && !K_new && !V_new) || !cu_q || !seq_lens || !block_table) return HGA_ERR_NULL;      // (a tensor of no rows may have no address)
   if ((K_new && (!K_cache || (scaled && !K_scale))) || (V_new && (!V_cache || (scaled && !V_scale)))) return HGA_ERR_NULL;
   if (misaligned(K_new) || misaligned(V_new) || misaligned(K_cache) || misaligned(V_cache) || misaligned(K_scale) || misaligned(V_scale) ||
-      misaligned(cu_q, 4) || misaligned(seq_lens, 4) || misaligned(block_table, 4))
+      misaligned(cu_q, 4) || misaligned(seq_lens, 4) || misaligned(block_table, 4) || misaligned(status_word, 4))
     return HGA_ERR_ALIGN;
   if (dm.n_tokens == 0) return HGA_OK;
   return launch_cache_write(dm, K_new, V_new, cu_q, seq_lens, block_table, K_cache, V_cache, K_scale, V_scale, status_word,
@@ -113,7 +113,7 @@ int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t tok_end
   if ((tok_end > tok_begin && !K_out && !V_out) || !seq_lens || !block_table) return HGA_ERR_NULL;
   if ((K_out && (!K_cache || (scaled && !K_scale))) || (V_out && (!V_cache || (scaled && !V_scale)))) return HGA_ERR_NULL;
   if (misaligned(K_out) || misaligned(V_out) || misaligned(K_cache) || misaligned(V_cache) || misaligned(K_scale) || misaligned(V_scale) ||
-      misaligned(seq_lens, 4) || misaligned(block_table, 4))
+      misaligned(seq_lens, 4) || misaligned(block_table, 4) || misaligned(status_word, 4))
     return HGA_ERR_ALIGN;
   if (tok_begin < 0 || tok_end < tok_begin || tok_end > 0x7fffff00) return HGA_ERR_SHAPE;      // (rows of the last CTA are counted in an int)
   const int64_t n = tok_end - tok_begin, d = dm.d, dense[3] = {dm.Hkv * n * d, n * d, d};
@@ -134,7 +134,7 @@ int hga_cache_attn(const hga_cache_params* p, const void* Q, const int32_t* cu_q
   if ((dm.n_tokens > 0 && (!Q || !O)) || !cu_q || !seq_lens || !block_table || !K_cache || !V_cache) return HGA_ERR_NULL;
   if (dm.format != HGA_CACHE_BF16 && (!K_scale || !V_scale)) return HGA_ERR_NULL;
   if (misaligned(Q) || misaligned(K_cache) || misaligned(V_cache) || misaligned(K_scale) || misaligned(V_scale) || misaligned(O) ||
-      misaligned(LSE, 4) || misaligned(cu_q, 4) || misaligned(seq_lens, 4) || misaligned(block_table, 4))
+      misaligned(LSE, 4) || misaligned(cu_q, 4) || misaligned(seq_lens, 4) || misaligned(block_table, 4) || misaligned(status_word, 4))
     return HGA_ERR_ALIGN;
   const CacheSplit sp = attn_split(dm);
   const size_t need = sp.bytes(dm);

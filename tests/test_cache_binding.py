@@ -73,3 +73,13 @@ def test_strides_are_named_for_every_argument():
         want = {"K_new": "kn_stride", "V_new": "vn_stride", "block_table": "table_stride", "K_cache": "k_stride", "V_cache": "v_stride",
                 "K_out": "out_stride", "V_out": "out_stride", "Q": "q_stride", "O": "o_stride"}
         assert strides == tuple(want.get(n) for n in names)
+
+
+def test_a_misaligned_status_word_is_refused(lib, ptr):
+    """it is written by an atomic, which faults there (no launch here: refused ahead of it)"""
+    p = params(n_tokens=0)
+    for off in (1, 2, 3):
+        assert lib.hga_cache_write(C.byref(p), *[ptr] * 9, ptr + off, None) == -3
+        assert lib.hga_cache_attn(C.byref(p), *[ptr] * 10, None, 0, ptr + off, None) == -3
+        assert lib.hga_cache_read(C.byref(p), 7, 7, *[ptr] * 8, ptr + off, None) == -3
+    assert lib.hga_cache_write(C.byref(p), *[ptr] * 9, ptr + 4, None) == 0
