@@ -338,7 +338,8 @@ typedef struct hga_cache_params {
   int32_t n_tokens;                               /* rows of the packed tensors (all new tokens together)        */
   int32_t max_new;                                /* no sequence has more new tokens than this (>= 1)            */
   int32_t max_len;                                /* no seq_lens entry is larger than this; 0 = max_pages * page_size.  The
-                                                     closer, the better the work is shared out.  The smaller of the two: 2^30 at most */
+                                                     closer, the better the work is shared out, which follows the
+                                                     limit and not the lengths.  The smaller of the two: 2^30 at most */
   float   softmax_scale;                          /* <= 0 selects 1/sqrt(head_dim)                               */
   int32_t flags;                                  /* 0                                                           */
   int32_t reserved;                               /* 0                                                           */
@@ -371,18 +372,18 @@ HGA_API int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t
  * row does not see have no influence on it, not even infinities or NaN, but for one: newer tokens may decide how probabilities are rounded.
  * Products are of bf16 numbers (the cache's are), sums in fp32, powers of two within 2^-18 of themselves.  Probabilities are rounded
  *   over a bf16 pool      to bf16: off by 2^-8 of themselves
- *   over a quantised one  to fp16: off by 2^-11 of themselves or 2^-31 of the row's largest; or to bf16 where scales of blocks that are not all
- *                         zeros lie outside 2^-18 .. 2^1 (e4m3), 2^-16 .. 2^9 (e2m1): with up to 48 or 64 new tokens x Hq/Hkv, all with a V
- *                         scale of that kind among the same 32 keys; with more, all of up to 256 such rows if any key up to the last one's has it in
- *                         K or V.  (These rows are computed twice: a chunk with a scale of that kind in its history takes twice as long or more.)
+ *   over a quantised one  to fp16: off by 2^-11 of themselves or 2^-31 of the row's largest; or to bf16 where the scale of a block that is not
+ *                         all zeros lies outside 2^-18 .. 2^1 (e4m3), 2^-16 .. 2^9 (e2m1).  If max_new * Hq/Hkv <= 64, a V scale of that kind
+ *                         decides so for the 32 keys around it; otherwise one of K or V does for a unit of up to 256 rows (new tokens x Hq/Hkv)
+ *                         if any of these sees it.  Such a unit is computed a second time: the call takes about 2.5 times as long where all are.
  * Numbers of a quantised pool below 2^-118 count as zeros, and of a query row over one those that are below 2^-29 of its largest or 2^-117
  * lose bits.
  * Results do not depend on what else is in the batch, nor change from run to run, except that the numbers in the parameters (n_seq, n_tokens,
  * max_new, max_len and the like) decide how the keys are shared out.
  * Sizes: logits (after the scale) below 2^24 in magnitude; the number of keys times the largest |V| below 2^108; in a quantised pool |K| below
  * 2^100.  Beyond these, sums may overflow: rows of that sequence may be infinite or NaN.
- * workspace: device scratch of at least hga_cache_workspace_bytes() bytes (16-byte aligned; may be NULL where that is 0); contents
- * are overwritten.  Calls that share a workspace must not overlap. */
+ * workspace: device scratch of at least hga_cache_workspace_bytes() bytes (16-byte aligned; may be NULL where that is 0; it grows with max_len where
+ * keys are shared out); contents are overwritten.  Calls that share a workspace must not overlap. */
 HGA_API int hga_cache_attn(const hga_cache_params* p, const void* Q, const int32_t* cu_q, const int32_t* seq_lens,
                            const int32_t* block_table, const void* K_cache, const void* V_cache, const void* K_scale,
                            const void* V_scale, void* O, float* LSE, void* workspace, size_t workspace_bytes,

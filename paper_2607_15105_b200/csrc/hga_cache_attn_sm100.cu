@@ -14,15 +14,16 @@
 //
 // Quantised pages are multiplied as fp16, into which the converter instructions go and which holds e4m3 and e2m1 with their scales
 // exactly while these lie in a range of 2^22 (e4m3; Q is brought to fp16 by a power of two per row, exactly but for numbers 2^-29 of
-// the row's largest).  A unit that meets another scale starts again in bf16.
+// the row's largest).  A unit that meets another scale starts again in bf16, when it has come to its end: one block of values below 8e-4 in a
+// history is enough (12 packed sequences, e4m3, with one each: 541 us -> 1353).
 //
 // A hidden key has weight zero, which does not silence a V row that is not finite.  So in the tiles that hold keys hidden from the
 // unit's first row (the last ones), numbers that are not finite are replaced by zeros, rows behind the last key altogether, and the
-// rows that do see such numbers get them added at the end.
+// rows that do see such numbers get them added at the end.  (Of quantised pages: blocks with a scale of 255, and e4m3's NaN codes.)
 //
-// Measured, 32 query heads on 8 of 128: 2048 tokens behind 14336, bf16, 472 to 540 us from one machine to another (0.95 to 1.09 PFLOP/s; tensor
-// pipe active 71 % of the time, 256 units on 148 SMs); 16384 tokens 1870 to 2190 us (1.00 to 1.18 PFLOP/s, at the power limit); e4m3, 12 packed
-// sequences 538 to 561 us (0.82 to 0.86 PFLOP/s: the shared-memory pipe, 77 to 85 % busy with converted tiles and the GEMMs' operands).
+// Measured, 32 query heads on 8 of 128, calls one after another: 2048 tokens behind 14336, bf16, 538 to 545 us (0.95 PFLOP/s; tensor pipe active
+// 71 % of the time, 256 units on 148 SMs); 16384 tokens 2176 to 2205 us (1.0 PFLOP/s, at the power limit); e4m3, 12 packed sequences 541 to 570 us (0.81 to 0.85 PFLOP/s: the shared-memory pipe, 77 to 85 % busy with converted tiles and the GEMMs'
+// operands), e2m1 509.
 #include <algorithm>
 #include <atomic>
 #include <cmath>

@@ -14,15 +14,15 @@
 // Quantised pages are multiplied as fp16, into which the converter instructions go, and which holds e4m3 and e2m1 exactly.  K without
 // its scales: they multiply the sums over a block (fp32) afterwards; Q is brought to fp16 by a power of two per row, exactly but for
 // numbers 2^-29 of the row's largest.  V with its scales, times 2^kLift, where all of a step's lie in fp16's range (of blocks
-// between 2^-12 and 2^9 in magnitude, e4m3); other steps go through bf16, exactly too, and slower.
+// between 2^-12 and 2^9 in magnitude, e4m3; blocks of zeros need none); other steps go through bf16, exactly too, and slower.
 //
 // Softmax: every warp has one reference per row, raised (and its sums rescaled) only when a logit exceeds it by 2^14, so that most
 // steps have no exchange between lanes.  It stays 2^6 below the row's largest when it is raised: fp16 then keeps weights down to 2^-31.
 // LSE is of the exact probabilities; O is divided by the sum of the rounded ones, a product with a column of ones.
 //
-// Measured, 32 query heads on 8 of 128, one token: bf16, 65533 keys 48.5 us (5.5 TB/s, 84 % of a copy's rate); 32 sequences of 16K bf16 318 us
-// (6.7 TB/s), e4m3 207 us (5.3 TB/s), e2m1 143 us (4.1 TB/s): what has fewer bytes is bound by the conversion's instructions (45 to 53 % of the
-// issue slots at three CTAs of four warps per SM).
+// Measured, 32 query heads on 8 of 128, one token: bf16, 65533 keys 48.8 us (5.5 TB/s, 84 % of a copy's rate); 32 sequences of 16K bf16 316 us
+// (6.8 TB/s), e4m3 202 to 220 us from one machine to another (5.0 to 5.5 TB/s), e2m1 143 us (4.0 TB/s).  What has fewer bytes leaves every unit below
+// its limit (e4m3: HBM 54 %, issue slots 45 %): latency, with three CTAs of four warps per SM, each with one step of copies ahead.
 #include <algorithm>
 #include <type_traits>
 
