@@ -372,10 +372,11 @@ HGA_API int hga_cache_read(const hga_cache_params* p, int32_t tok_begin, int32_t
  * row does not see have no influence on it, not even infinities or NaN, but for one: newer tokens may decide how probabilities are rounded.
  * Products are of bf16 numbers (the cache's are), sums in fp32, powers of two within 2^-18 of themselves.  Probabilities are rounded
  *   over a bf16 pool      to bf16: off by 2^-8 of themselves
- *   over a quantised one  to fp16: off by 2^-11 of themselves or 2^-31 of the row's largest; or to bf16 where the scale of a block that is not
- *                         all zeros lies outside 2^-18 .. 2^1 (e4m3), 2^-16 .. 2^9 (e2m1).  If max_new * Hq/Hkv <= 64, a V scale of that kind
- *                         decides so for the 32 keys around it; otherwise one of K or V does for a unit of up to 256 rows (new tokens x Hq/Hkv)
- *                         if any of these sees it.  Such a unit is computed a second time: the call takes about 2.5 times as long where all are.
+ *   over a quantised one  to fp16: off by 2^-11 of themselves or 2^-31 of the row's largest.  To bf16, however, if the scale of a block that
+ *                         is not all zeros is out of fp16's range, which holds 2^-18 .. 2^1 (e4m3), 2^-16 .. 2^9 (e2m1) at least: where
+ *                         max_new * Hq/Hkv <= 64, a V scale of that kind decides so for the 32 keys around it; otherwise one of K or V
+ *                         does for a unit of up to 256 rows (new tokens x Hq/Hkv) if any of these sees it.  Such a unit is computed a
+ *                         second time: the call takes about 2.5 times as long where all are.
  * Numbers of a quantised pool below 2^-118 count as zeros, and of a query row over one those that are below 2^-29 of its largest or 2^-117
  * lose bits.
  * Results do not depend on what else is in the batch, nor change from run to run, except that the numbers in the parameters (n_seq, n_tokens,

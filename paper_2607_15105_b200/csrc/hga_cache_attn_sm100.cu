@@ -21,9 +21,9 @@
 // unit's first row (the last ones), numbers that are not finite are replaced by zeros, rows behind the last key altogether, and the
 // rows that do see such numbers get them added at the end.  (Of quantised pages: blocks with a scale of 255, and e4m3's NaN codes.)
 //
-// Measured, 32 query heads on 8 of 128, calls one after another: 2048 tokens behind 14336, bf16, 538 to 545 us (0.95 PFLOP/s; tensor pipe active
-// 71 % of the time, 256 units on 148 SMs); 16384 tokens 2176 to 2205 us (1.0 PFLOP/s, at the power limit); e4m3, 12 packed sequences 541 to 570 us (0.81 to 0.85 PFLOP/s: the shared-memory pipe, 77 to 85 % busy with converted tiles and the GEMMs'
-// operands), e2m1 509.
+// Measured, 32 query heads on 8 of 128, calls one after another: 2048 tokens behind 14336, bf16, 534 to 545 us (0.95 PFLOP/s; tensor pipe active
+// 71 % of the time, 256 units on 148 SMs); 16384 tokens 2159 to 2205 us (1.0 PFLOP/s, at the power limit); e4m3, 12 packed sequences 541 to
+// 570 us (0.81 to 0.85 PFLOP/s: the shared-memory pipe, 76 to 85 % busy with converted tiles and the GEMMs' operands), e2m1 509.
 #include <algorithm>
 #include <atomic>
 #include <cmath>

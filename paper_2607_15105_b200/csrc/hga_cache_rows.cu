@@ -22,7 +22,7 @@
 //
 // Measured, 32 query heads on 8 of 128, one token: bf16, 65533 keys 48.8 us (5.5 TB/s, 84 % of a copy's rate); 32 sequences of 16K bf16 316 us
 // (6.8 TB/s), e4m3 202 to 220 us from one machine to another (5.0 to 5.5 TB/s), e2m1 143 us (4.0 TB/s).  What has fewer bytes leaves every unit below
-// its limit (e4m3: HBM 54 %, issue slots 45 %): latency, with three CTAs of four warps per SM, each with one step of copies ahead.
+// its limit (e4m3: HBM 54 %, issue slots 44 %): latency, with three CTAs of four warps per SM, each with one step of copies ahead.
 #include <algorithm>
 #include <type_traits>
 

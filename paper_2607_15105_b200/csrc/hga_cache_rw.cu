@@ -4,8 +4,8 @@
 // V, and several rows: the lanes of a row access whole sectors on both sides, and where a row lies is worked out once for the four pieces.
 //
 // Measured, 8 heads of 128, calls one after another: 16384 tokens written in e4m3 in 20.0 to 20.8 us (102 MB, 4.9 to 5.1 TB/s; 72 % of the issue
-// slots), in bf16 23.2 us (134 MB, 88 % of a copy's rate); 4 x 16384 read in e4m3 in 65.4 to 66.2 us (407 MB, 6.2 TB/s, 94 %), in e2m1 56.0 (92 %), in
-// bf16 83.9 (97 %).  One token each of 32 sequences: 9.1 to 9.8 us, of which the kernel has little more than the launch.
+// slots), in bf16 23.2 us (134 MB, 88 % of a copy's rate); 4 x 16384 read in e4m3 in 65.4 to 66.2 us (407 MB, 6.2 TB/s, 94 %), in e2m1 56.0
+// (92 %), in bf16 83.9 (97 %).  One token each of 32 sequences: 9.1 to 9.8 us, of which the kernel has little more than the launch.
 #include "hga_cache.cuh"
 #include "hga_sm100.cuh"
 
